@@ -408,6 +408,109 @@ dybit_status dybit_search(int32_t n_layers, const double *lat, const double *rms
                           int32_t strategy, double constraint, int32_t k,
                           int32_t *w_bits_out, int32_t *a_bits_out, double *ratio_out, int32_t *met_out);
 
+/* ---- a key/value cache of codes ---------------------------------------------------------------------------------
+ * What a decoder of a language model keeps between its steps: the keys and values of every token, as signed DyBit
+ * codes of 4 or 8 bits with one fp32 scale per token and head, in pages that sequences own or share.
+ *
+ * Heads of a batch of tokens, as a (fused) projection leaves them: element (token t, head h, d) is
+ * data[t * token_stride + h * head_stride + d].  Strides count elements; any stride is allowed for an input, for an output
+ * the heads must not overlap.  tokens == 0 is valid (nothing is done). */
+typedef enum { DYBIT_F32 = 0, DYBIT_F16 = 1, DYBIT_BF16 = 2 } dybit_type;
+typedef struct {
+    void *data;            /* [device] aligned to its element                                                 */
+    int64_t tokens, token_stride, head_stride;
+    int32_t heads, head_dim, type;                                               /* type: a dybit_type */
+} dybit_heads;
+
+/* The cache of one layer (of all layers, one after the other, for dybit_kv_copy_pages).  All arrays [device], 16-byte aligned:
+ *   k_codes, v_codes    [layers][pages][heads][page_tokens][head_dim * bits / 8]
+ *   k_scales, v_scales  [layers][pages][heads][page_tokens]
+ * k_fmt, v_fmt: signed, 4 or 8 bits each (DYBIT_ERR_UNSUPPORTED_BITS otherwise).  head_dim 64, 128 or 256 (smaller heads are
+ * stored with zeros behind them: a zero changes no score and no scale); page_tokens a power of two, 16 to 1024; pages < 2^31.
+ * What lies behind the last token of a sequence in its last page does not matter, whatever its bits. */
+typedef struct {
+    uint8_t *k_codes;
+    float *k_scales;
+    uint8_t *v_codes;
+    float *v_scales;
+    int64_t layers, pages;
+    int32_t heads, page_tokens, head_dim;
+    dybit_fmt k_fmt, v_fmt;
+} dybit_kv_cache;
+
+/* RMS norm of every query head and every key head, and the rotation by the token's position, in one pass:
+ *     n = x / sqrt(mean(x^2) + eps) * weight          (over the head_dim elements of one head)
+ *     (a, b) -> (a cos - b sin, b cos + a sin)        on `rotary` / 2 pairs of the first `rotary` elements of n
+ * with pair i = (i, i + rotary / 2), or, neighbours = 1, (2i, 2i + 1); the elements behind them pass unturned.  Computed in
+ * fp32, rounded once to the type of the output.
+ *   q, k       [device] any of the three types, the same for all of them; k.heads 0: queries only.  head_dim even, 2 to 512.
+ *   q_weight, k_weight  [device] head_dim floats
+ *   positions  [device] q.tokens integers; cos_table, sin_table [device]: table_rows rows of rotary / 2 floats, row = position.
+ *              A position outside the table: the token's outputs are NaN and the asynchronous error flag is set
+ *              (DYBIT_ERR_INVALID_ARG).
+ *   rotary     even, 2 to head_dim.  eps >= 0.
+ *   q_out, k_out  may be q and k themselves (same data and strides), else must not overlap any input. */
+dybit_status dybit_head_norm_rope(dybit_heads q, dybit_heads k, const float *q_weight, const float *k_weight,
+                                  const int64_t *positions, const float *cos_table, const float *sin_table, int64_t table_rows,
+                                  int32_t rotary, int32_t neighbours, float eps, dybit_heads q_out, dybit_heads k_out,
+                                  dybit_stream stream);
+
+/* Its gradient: from grad_q, grad_k (of the outputs) and the forward's inputs, those of the inputs, dq and dk, and of the
+ * weights (sums over tokens and heads, written, not added to; the order of the additions is fixed).  A token whose position is
+ * outside the table gets NaN and adds nothing to the weights' gradients.  dq, dk may be grad_q, grad_k themselves.
+ *   workspace  [device] dybit_head_norm_rope_bwd_workspace(q.tokens, q.heads + k.heads, head_dim) floats, 16-byte aligned */
+size_t dybit_head_norm_rope_bwd_workspace(int64_t tokens, int32_t heads, int32_t head_dim);
+dybit_status dybit_head_norm_rope_bwd(dybit_heads grad_q, dybit_heads grad_k, dybit_heads q, dybit_heads k,
+                                      const float *q_weight, const float *k_weight, const int64_t *positions,
+                                      const float *cos_table, const float *sin_table, int64_t table_rows,
+                                      int32_t rotary, int32_t neighbours, float eps, dybit_heads dq, dybit_heads dk,
+                                      float *q_weight_grad, float *k_weight_grad, float *workspace, dybit_stream stream);
+
+/* New keys and values into the cache: for token t and every head, the scale max|x| / 2^(m-1) (1.0 for a maximum of 0) and the
+ * codes of dybit_quantize under it go to place slots[t] = page * page_tokens + place in the page.  Slots of one call must differ;
+ * a negative slot skips its token, one past the pool skips it and sets the asynchronous error flag (DYBIT_ERR_INVALID_ARG).
+ * NaNs are ignored by the maximum and stored as zero.  A head whose scale would be subnormal is stored as zeros with scale 1; one
+ * whose maximum is infinite as zeros with scale NaN (so attention that sees it returns NaN), with the error flag set
+ * (DYBIT_ERR_BAD_SCALE).
+ *   keys, values  [device] keys.tokens tokens of cache.heads heads of cache.head_dim; cache.layers is 1 */
+dybit_status dybit_kv_append(dybit_heads keys, dybit_heads values, const int64_t *slots, dybit_kv_cache cache, dybit_stream stream);
+
+/* Page src[i] of every layer copied over page dst[i], codes and scales of keys and values, for i < n: what forking a sequence
+ * inside a page and compacting a pool come down to.  The pages of dst must differ from each other and from those of src.  A page
+ * number outside the pool copies nothing and sets the asynchronous error flag (DYBIT_ERR_INVALID_ARG).  src, dst [device]. */
+dybit_status dybit_kv_copy_pages(dybit_kv_cache cache, const int32_t *src, const int32_t *dst, int64_t n, dybit_stream stream);
+
+/* Tokens that consecutive sequences of a batch share in front of their own: group g, sequences starts[g] to starts[g + 1] - 1, sees
+ * the first lengths[g] tokens of the pages in row g of tables.  Read and multiplied once for all queries of the group.
+ * groups == 0: none.  max_queries: no group has more query tokens (its sequences' together).  max_length: see
+ * dybit_kv_attention.  Sequences that no group names see no prefix. */
+typedef struct {
+    const int32_t *tables;      /* [device] groups rows of table_width page numbers */
+    const int32_t *lengths;     /* [device] groups                                  */
+    const int32_t *starts;      /* [device] groups + 1, ascending                   */
+    int64_t groups, table_width, max_queries, max_length;
+} dybit_kv_prefix;
+
+/* Attention of new tokens over the cache, softmax(scale * q K^T) V with queries' heads in groups of q.heads / cache.heads per key
+ * head.  The queries of sequence s are tokens starts[s] to starts[s + 1] - 1 of q (starts NULL: token s alone); its keys the
+ * lengths[s] tokens in the pages that row s of tables names, the new ones, appended before, among them.  causal: query i of n sees
+ * the keys before lengths[s] - (n - 1 - i); otherwise all.  Every query sees its group's prefix.  A query that sees nothing gets
+ * zeros.  Scores, maxima and sums are held in fp32.
+ *   q, out     [device] of one type; out must not overlap anything else
+ *   tables     [device] `sequences` rows of table_width page numbers, read as far as lengths say.  A page number outside the pool,
+ *              or a length past the table, leaves those tokens out and sets the asynchronous error flag (DYBIT_ERR_INVALID_ARG).
+ *   max_queries   no sequence has more query tokens (queries past it are not computed, and the flag is set)
+ *   max_length    0, or a bound on lengths that the caller knows: how the work is split goes by it (0: the table's width), the
+ *                 result does not depend on it.  Keys past it are left out, with the flag set.
+ * Rows of out that belong to no sequence are not written.
+ *   workspace  [device] 16-byte aligned, dybit_kv_attention_workspace_bytes(...) bytes (0: may be NULL); contents do not matter. */
+size_t dybit_kv_attention_workspace_bytes(dybit_heads q, dybit_kv_cache cache, int64_t table_width, int64_t sequences, int64_t max_queries,
+                                          int64_t max_length, dybit_kv_prefix prefix);
+dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, const int32_t *tables, int64_t table_width, const int32_t *lengths,
+                                const int32_t *starts, int64_t sequences, int64_t max_queries, int64_t max_length, int32_t causal,
+                                float scale, dybit_kv_prefix prefix, dybit_heads out, uint8_t *workspace, size_t workspace_bytes,
+                                dybit_stream stream);
+
 /* Waits for `stream`, then reports and clears the asynchronous error flag of the current
  * device: *flag_out [host] is DYBIT_OK or DYBIT_ERR_BAD_SCALE (a dybit_quantize kernel since the
  * last call, or a write-back epilogue, found an unusable scale and wrote no codes, or a dybit_absmax_scale_ws

@@ -12,6 +12,7 @@ import ctypes as C
 import operator
 import os
 import warnings
+from typing import NamedTuple
 
 import torch  # imported first so that the library binds to the HIP runtime torch already loaded
 
@@ -24,6 +25,47 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED_BITS, ERR_BAD_SCALE, ERR_ALIGNMENT, ERR_NULL, E
 
 class Fmt(C.Structure):
     _fields_ = [("bits", C.c_int32), ("is_signed", C.c_int32)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("tokens", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("heads", C.c_int32), ("head_dim", C.c_int32), ("type", C.c_int32)]
+
+
+class KVCacheStruct(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+                ("layers", C.c_int64), ("pages", C.c_int64), ("heads", C.c_int32), ("page_tokens", C.c_int32), ("head_dim", C.c_int32),
+                ("k_fmt", Fmt), ("v_fmt", Fmt)]
+
+
+class KVPrefixStruct(C.Structure):
+    _fields_ = [("tables", C.c_void_p), ("lengths", C.c_void_p), ("starts", C.c_void_p), ("groups", C.c_int64), ("table_width", C.c_int64),
+                ("max_queries", C.c_int64), ("max_length", C.c_int64)]
+
+
+class KVCache(NamedTuple):
+    """Pages of keys and values as signed DyBit codes: codes [pages][heads][page_tokens][head_dim * bits / 8] (uint8), scales
+    [pages][heads][page_tokens] (float32); with one more dimension in front, all layers of a model (`layer` picks one)."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    k_bits: int
+    v_bits: int
+
+    def layer(self, i: int) -> "KVCache":
+        return KVCache(self.k_codes[i], self.k_scales[i], self.v_codes[i], self.v_scales[i], self.k_bits, self.v_bits)
+
+
+class SharedPrefix(NamedTuple):
+    """Tokens that consecutive sequences of a batch see in front of their own: row g of `tables` (int32 [groups][pages]) and
+    `lengths` (int32 [groups]) for the sequences starts[g] to starts[g + 1] - 1 (int32 [groups + 1]).  max_queries: most query
+    tokens that a group has, its sequences' together; max_length: 0 or a bound on `lengths`."""
+    tables: torch.Tensor
+    lengths: torch.Tensor
+    starts: torch.Tensor
+    max_queries: int
+    max_length: int = 0
 
 
 class DybitError(RuntimeError):
@@ -67,6 +109,32 @@ class _Ctypes:
 
     def dybit_packed_bytes(self, pair, n):
         return int(lib().dybit_packed_bytes(fmt(*pair), n))
+
+    def dybit_head_norm_rope(self, q, k, q_weight, k_weight, positions, cos, sin, rows, rotary, neighbours, eps, q_out, k_out, stream):
+        return lib().dybit_head_norm_rope(_heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _typed(positions, torch.int64), _ptr(cos), _ptr(sin),
+                                          rows, rotary, neighbours, eps, _heads(q_out), _heads(k_out), _stream(stream))
+
+    def dybit_head_norm_rope_bwd(self, gq, gk, q, k, q_weight, k_weight, positions, cos, sin, rows, rotary, neighbours, eps, dq, dk, dwq, dwk, work,
+                                 stream):
+        return lib().dybit_head_norm_rope_bwd(_heads(gq), _heads(gk), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _typed(positions, torch.int64),
+                                              _ptr(cos), _ptr(sin), rows, rotary, neighbours, eps, _heads(dq), _heads(dk), _ptr(dwq), _ptr(dwk),
+                                              _ptr(work), _stream(stream))
+
+    def dybit_kv_append(self, keys, values, slots, cache, stream):
+        return lib().dybit_kv_append(_heads(keys), _heads(values), _typed(slots, torch.int64), _kv_cache(cache), _stream(stream))
+
+    def dybit_kv_copy_pages(self, cache, src, dst, n, stream):
+        return lib().dybit_kv_copy_pages(_kv_cache(cache), _typed(src, torch.int32), _typed(dst, torch.int32), n, _stream(stream))
+
+    def dybit_kv_attention(self, q, cache, tables, width, lengths, starts, sequences, max_queries, max_length, causal, scale, prefix, out):
+        x, c, h = _kv_prefix(prefix), _kv_cache(cache), _heads(q)
+        need = int(lib().dybit_kv_attention_workspace_bytes(h, c, width, sequences, max_queries, max_length, x))
+        work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        return lib().dybit_kv_attention(h, c, _typed(tables, torch.int32), width, _typed(lengths, torch.int32), _typed(starts, torch.int32), sequences,
+                                        max_queries, max_length, bool(causal), scale, x, _heads(out), _ptr(work), need, _stream())
+
+    def empty_rows(self, like):
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
 
     def empty(self, like, floats, *sizes):
         return torch.empty(sizes, dtype=torch.float32 if floats else torch.uint8, device=like.device)
@@ -114,6 +182,16 @@ def lib() -> C.CDLL:
         L.dybit_quantize_cols.argtypes = [vp, i64, i64, Fmt, vp, vp, vp]
         L.dybit_dwconv2d_wb.argtypes = [i64] * 4 + [i32] * 4 + [vp, Fmt, vp, vp, Fmt, vp, i32, vp, i32, vp, vp, Fmt, vp, vp, vp]
         L.dybit_group_conv2d.argtypes = [i64] * 5 + [i32] * 5 + [vp, Fmt, vp, vp, Fmt, vp, i32, vp, vp, i32, vp, vp, vp]
+        f32 = C.c_float
+        L.dybit_head_norm_rope.argtypes = [Heads, Heads, vp, vp, vp, vp, vp, i64, i32, i32, f32, Heads, Heads, vp]
+        L.dybit_head_norm_rope_bwd_workspace.argtypes = [i64, i32, i32]
+        L.dybit_head_norm_rope_bwd_workspace.restype = sz
+        L.dybit_head_norm_rope_bwd.argtypes = [Heads] * 4 + [vp] * 5 + [i64, i32, i32, f32, Heads, Heads, vp, vp, vp, vp]
+        L.dybit_kv_append.argtypes = [Heads, Heads, vp, KVCacheStruct, vp]
+        L.dybit_kv_copy_pages.argtypes = [KVCacheStruct, vp, vp, i64, vp]
+        L.dybit_kv_attention_workspace_bytes.argtypes = [Heads, KVCacheStruct, i64, i64, i64, i64, KVPrefixStruct]
+        L.dybit_kv_attention_workspace_bytes.restype = sz
+        L.dybit_kv_attention.argtypes = [Heads, KVCacheStruct, vp, i64, vp, vp, i64, i64, i64, i32, f32, KVPrefixStruct, Heads, vp, sz, vp]
         L.dybit_search.argtypes = [i32, vp, vp, vp, i32, C.c_double, i32, vp, vp, C.POINTER(C.c_double), C.POINTER(i32)]
         L.dybit_get_last_async_error.argtypes = [C.POINTER(i32), vp]
         L.dybit_set_async_error_word.argtypes = [vp]
@@ -154,6 +232,47 @@ def _ptr(t) -> int | None:
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
     return t.data_ptr()
+
+
+def _typed(t, dtype) -> int | None:
+    if t is not None and t.dtype != dtype:
+        raise TypeError(f"expected a tensor of {str(dtype).replace('torch.', '')}")
+    return _ptr(t)
+
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _heads(t) -> Heads:
+    if t is None:
+        return Heads()
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dim() != 3:
+        raise ValueError("expected a tensor [tokens][heads][head_dim]")
+    if t.stride(2) != 1 and t.shape[2] > 1 and t.numel():
+        raise ValueError("expected heads whose elements are contiguous")
+    if t.dtype not in _TYPES:
+        raise TypeError("expected float32, float16 or bfloat16")
+    return Heads(t.data_ptr(), t.shape[0], t.stride(0), t.stride(1), t.shape[1], t.shape[2], _TYPES[t.dtype])
+
+
+def _kv_cache(cache) -> KVCacheStruct:
+    k, ks, v, vs, kb, vb = cache
+    p = [_typed(t, d) for t, d in ((k, torch.uint8), (ks, torch.float32), (v, torch.uint8), (vs, torch.float32))]
+    D = k.shape[-1] * 8 // kb if kb > 0 and vb > 0 else 0
+    if k.dim() not in (4, 5) or not k.shape[:-1] == v.shape[:-1] == ks.shape == vs.shape or k.shape[-1] * 8 != D * kb or v.shape[-1] * 8 != D * vb:
+        raise ValueError("the tensors of a KVCache do not belong together")
+    return KVCacheStruct(*p, k.shape[0] if k.dim() == 5 else 1, *k.shape[-4:-1], D, fmt(kb, True), fmt(vb, True))
+
+
+def _kv_prefix(prefix) -> KVPrefixStruct:
+    if prefix is None:
+        return KVPrefixStruct()
+    tables, lengths, starts, max_queries, max_length = prefix
+    if tables.dim() != 2 or lengths.numel() != tables.shape[0] or starts.numel() != tables.shape[0] + 1:
+        raise ValueError("the tensors of a SharedPrefix do not belong together")
+    return KVPrefixStruct(*(_typed(t, torch.int32) for t in (tables, lengths, starts)), *tables.shape, max_queries, max_length)
 
 
 # ---- host-only --------------------------------------------------------------
@@ -605,3 +724,81 @@ def dybit_diag_mfma_f6(operands: torch.Tensor, workgroups: int, iters: int, sink
     _check(lib().dybit_diag_mfma_f6(_ptr(operands), workgroups, iters, _ptr(sink), C.byref(flops), _stream(stream)),
            "dybit_diag_mfma_f6")
     return float(flops.value)
+
+
+# ---- a key/value cache of codes ---------------------------------------------
+def dybit_head_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight: torch.Tensor, k_weight: torch.Tensor | None, positions: torch.Tensor,
+                         cos: torch.Tensor, sin: torch.Tensor, eps: float = 1e-6, neighbours: bool = False, out=None, stream=None):
+    """RMS norm of every head of q and k ([tokens][heads][head_dim], float32, float16 or bfloat16, any strides over tokens and
+    heads) and the rotation by positions (int64 [tokens]) of its first 2 * cos.shape[1] elements; cos, sin: float32 [positions]
+    [pairs].  neighbours: pairs are neighbouring elements, not halves.  out: (q_out, k_out), which may be (q, k).
+    Returns (q_out, k_out)."""
+    q_out, k_out = out if out is not None else (_n().empty_rows(q), None if k is None else _n().empty_rows(k))
+    _check_rotation(q, q_weight, k, k_weight, positions, cos, sin)
+    _check(_n().dybit_head_norm_rope(q, k, q_weight, k_weight, positions, cos, sin, cos.shape[0], 2 * cos.shape[1], bool(neighbours), eps,
+                                     q_out, k_out, stream), "dybit_head_norm_rope")
+    return q_out, k_out
+
+
+def _check_rotation(q, q_weight, k, k_weight, positions, cos, sin):
+    assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and q_weight.dtype == torch.float32
+    if cos.dim() != 2 or cos.shape != sin.shape or positions.shape != q.shape[:1] or q_weight.numel() != q.shape[-1]:
+        raise ValueError("expected tables [positions][pairs], a position a token and a weight an element of a head")
+    if k is not None and (k_weight.dtype != torch.float32 or k_weight.numel() != k.shape[-1]):
+        raise ValueError("expected a float32 weight for every element of a key head")
+
+
+def dybit_head_norm_rope_bwd(grad_q: torch.Tensor, grad_k: torch.Tensor | None, q: torch.Tensor, k: torch.Tensor | None, q_weight: torch.Tensor,
+                             k_weight: torch.Tensor | None, positions: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor, eps: float = 1e-6,
+                             neighbours: bool = False, out=None, stream=None):
+    """Gradient of dybit_head_norm_rope from those of its outputs and its own inputs: (dq, dk, q_weight_grad, k_weight_grad), the last
+    two float32.  out: (dq, dk), which may be (grad_q, grad_k)."""
+    if stream is not None:                                   # the workspace has to be that stream's
+        with torch.cuda.stream(stream):
+            return dybit_head_norm_rope_bwd(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours, out)
+    _check_rotation(q, q_weight, k, k_weight, positions, cos, sin)
+    dq, dk = out if out is not None else (_n().empty_rows(q), None if k is None else _n().empty_rows(k))
+    D, heads = q.shape[2], q.shape[1] + (0 if k is None else k.shape[1])
+    dwq, dwk = _n().empty(q, True, D), None if k is None else _n().empty(q, True, D)
+    work = _n().empty(q, True, int(lib().dybit_head_norm_rope_bwd_workspace(q.shape[0], heads, D)))
+    _check(_n().dybit_head_norm_rope_bwd(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, cos.shape[0], 2 * cos.shape[1],
+                                         bool(neighbours), eps, dq, dk, dwq, dwk, work, None), "dybit_head_norm_rope_bwd")
+    return dq, dk, dwq, dwk
+
+
+def dybit_kv_append(keys: torch.Tensor, values: torch.Tensor, slots: torch.Tensor, cache: KVCache, stream=None) -> None:
+    """Encodes keys and values ([tokens][heads][head_dim]) into the places slots (int64 [tokens], page * page_tokens + place; negative:
+    skipped) of one layer's cache."""
+    if slots.numel() != keys.shape[0]:
+        raise ValueError("expected a slot for every token")
+    _check(_n().dybit_kv_append(keys, values, slots, cache, stream), "dybit_kv_append")
+
+
+def dybit_kv_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """Copies page src[i] over page dst[i] (int32, pages of dst all different and none of them in src) in every layer of the cache."""
+    n = src.numel()
+    if dst.numel() != n:
+        raise ValueError("expected as many pages to copy to as to copy from")
+    _check(_n().dybit_kv_copy_pages(cache, src, dst, n, stream), "dybit_kv_copy_pages")
+
+
+def dybit_kv_attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor | None = None,
+                       max_queries: int = 1, max_length: int = 0, causal: bool = True, scale: float | None = None,
+                       prefix: SharedPrefix | None = None, out: torch.Tensor | None = None, stream=None):
+    """Attention of q ([tokens][heads][head_dim]) over one layer's cache: sequence s has the query tokens starts[s] to starts[s + 1] - 1
+    (int32 [sequences + 1]; None: token s alone, at most max_queries each) and lengths[s] (int32) cached tokens, its new ones among
+    them, in the pages tables[s] (int32 [sequences][pages]).  max_length: 0 or a bound on `lengths`, by which the work is split.
+    scale: of the scores, None for 1 / sqrt(head_dim).  Rows of `out` that belong to no sequence are not written."""
+    if stream is not None:                                   # the workspace has to be that stream's
+        with torch.cuda.stream(stream):
+            return dybit_kv_attention(q, cache, tables, lengths, starts, max_queries, max_length, causal, scale, prefix, out)
+    n = lengths.numel()
+    if tables.dim() != 2 or tables.shape[0] != n or (q.shape[0] < n if starts is None else starts.numel() != n + 1):
+        raise ValueError("expected a row of pages, a length and query tokens for every sequence")
+    if out is None:
+        out = _n().empty_rows(q)
+    if scale is None:
+        scale = q.shape[2] ** -0.5
+    _check(_n().dybit_kv_attention(q, cache, tables, tables.shape[1], lengths, starts, n, max_queries, max_length, causal, scale, prefix, out),
+           "dybit_kv_attention")
+    return out

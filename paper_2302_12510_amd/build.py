@@ -98,6 +98,14 @@ SOURCES = [
     ("conv_patch.hip", "conv_patch_w2", ["-DDYBIT_PATCH_W=6"]),
     ("conv_patch.hip", "conv_patch_w2_wb", ["-DDYBIT_PATCH_W=6", "-DDYBIT_WB=1"]),
     ("conv_patch.hip", "conv_patch_w2_co", ["-DDYBIT_PATCH_W=6", "-DDYBIT_WB=2"]),
+    ("head_norm.hip", "head_norm", []),
+    ("kv_cache.hip", "kv_cache", []),
+    ("kv_attention_entry.hip", "kv_attention_entry", []),
+    # attention over the cache: one build per pair of code widths (keys, values)
+    ("kv_attention.hip", "kv_attention_k8v8", ["-DDYBIT_KV_K=8", "-DDYBIT_KV_V=8"]),
+    ("kv_attention.hip", "kv_attention_k8v4", ["-DDYBIT_KV_K=8", "-DDYBIT_KV_V=4"]),
+    ("kv_attention.hip", "kv_attention_k4v8", ["-DDYBIT_KV_K=4", "-DDYBIT_KV_V=8"]),
+    ("kv_attention.hip", "kv_attention_k4v4", ["-DDYBIT_KV_K=4", "-DDYBIT_KV_V=4"]),
     ("diag.hip", "diag", []),
 ]
 FLAGS = ["--offload-arch=gfx950", "--offload-compress", "-O3", "-fPIC", "-std=c++17",

@@ -101,8 +101,120 @@ dybit_fmt format(PyObject *o)
     return f;
 }
 
+// A tensor [tokens][heads][head_dim] of one of the three types, rows of heads contiguous; None: nothing.
+dybit_heads head_rows(PyObject *o)
+{
+    dybit_heads h{};
+    if (o == Py_None) return h;
+    if (!THPVariable_Check(o)) { PyErr_SetString(PyExc_TypeError, "expected a tensor"); throw PythonError(); }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) { PyErr_SetString(PyExc_ValueError, "expected a device tensor"); throw PythonError(); }
+    if (t.dim() != 3) { PyErr_SetString(PyExc_ValueError, "expected a tensor [tokens][heads][head_dim]"); throw PythonError(); }
+    if (t.stride(2) != 1 && t.size(2) > 1 && t.numel()) { PyErr_SetString(PyExc_ValueError, "expected heads whose elements are contiguous"); throw PythonError(); }
+    switch (t.scalar_type()) {
+        case at::kFloat: h.type = DYBIT_F32; break;
+        case at::kHalf: h.type = DYBIT_F16; break;
+        case at::kBFloat16: h.type = DYBIT_BF16; break;
+        default: PyErr_SetString(PyExc_TypeError, "expected float32, float16 or bfloat16"); throw PythonError();
+    }
+    if (t.size(1) > INT32_MAX || t.size(2) > INT32_MAX) { PyErr_SetString(PyExc_ValueError, "tensor too large"); throw PythonError(); }
+    h.data = t.data_ptr();
+    h.tokens = t.size(0); h.heads = (int32_t)t.size(1); h.head_dim = (int32_t)t.size(2);
+    h.token_stride = t.stride(0); h.head_stride = t.stride(1);
+    return h;
+}
+
+// A contiguous device tensor of one type; None: NULL.
+void *typed_address(PyObject *o, at::ScalarType type, const char *said)
+{
+    if (o != Py_None && THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() != type) { PyErr_Format(PyExc_TypeError, "expected a tensor of %s", said); throw PythonError(); }
+    return address(o);
+}
+
+// (k_codes, k_scales, v_codes, v_scales, k_bits, v_bits); codes [layers, where there are several][pages][heads][page_tokens][bytes].
+dybit_kv_cache kv_cache(PyObject *o)
+{
+    dybit_kv_cache c{};
+    PyObject *six = PySequence_Fast(o, "expected a KVCache");
+    if (!six) throw PythonError();
+    try {
+        if (PySequence_Fast_GET_SIZE(six) != 6) { PyErr_SetString(PyExc_TypeError, "expected a KVCache"); throw PythonError(); }
+        PyObject **f = PySequence_Fast_ITEMS(six);
+        for (int i = 0; i < 4; ++i)
+            if (!THPVariable_Check(f[i])) { PyErr_SetString(PyExc_TypeError, "a KVCache holds four tensors and two widths"); throw PythonError(); }
+        c.k_codes = (uint8_t *)typed_address(f[0], at::kByte, "uint8");
+        c.k_scales = (float *)typed_address(f[1], at::kFloat, "float32");
+        c.v_codes = (uint8_t *)typed_address(f[2], at::kByte, "uint8");
+        c.v_scales = (float *)typed_address(f[3], at::kFloat, "float32");
+        c.k_fmt = dybit_fmt{(int32_t)integer(f[4]), 1};
+        c.v_fmt = dybit_fmt{(int32_t)integer(f[5]), 1};
+        const at::Tensor &k = THPVariable_Unpack(f[0]), &ks = THPVariable_Unpack(f[1]), &v = THPVariable_Unpack(f[2]), &vs = THPVariable_Unpack(f[3]);
+        const int64_t n = k.dim();
+        bool fits = (n == 4 || n == 5) && v.dim() == n && ks.dim() == n - 1 && vs.dim() == n - 1;
+        for (int64_t i = 0; fits && i < n - 1; ++i) fits = k.size(i) == v.size(i) && k.size(i) == ks.size(i) && k.size(i) == vs.size(i);
+        if (fits && c.k_fmt.bits > 0 && c.v_fmt.bits > 0) {
+            c.head_dim = (int32_t)(k.size(n - 1) * 8 / c.k_fmt.bits);
+            fits = k.size(n - 1) * 8 == (int64_t)c.head_dim * c.k_fmt.bits && v.size(n - 1) * 8 == (int64_t)c.head_dim * c.v_fmt.bits &&
+                   k.size(n - 3) <= INT32_MAX && k.size(n - 2) <= INT32_MAX;
+        }
+        if (!fits) { PyErr_SetString(PyExc_ValueError, "the tensors of a KVCache do not belong together"); throw PythonError(); }
+        c.layers = n == 5 ? k.size(0) : 1;
+        c.pages = k.size(n - 4); c.heads = (int32_t)k.size(n - 3); c.page_tokens = (int32_t)k.size(n - 2);
+    } catch (const PythonError &) {
+        Py_DECREF(six);
+        throw;
+    }
+    Py_DECREF(six);
+    return c;
+}
+
+// (tables, lengths, starts, max_queries, max_length), None: no prefix.
+dybit_kv_prefix kv_prefix(PyObject *o)
+{
+    dybit_kv_prefix x{};
+    if (o == Py_None) return x;
+    PyObject *five = PySequence_Fast(o, "expected a SharedPrefix");
+    if (!five) throw PythonError();
+    try {
+        PyObject **f = PySequence_Fast_ITEMS(five);
+        if (PySequence_Fast_GET_SIZE(five) != 5 || !THPVariable_Check(f[0]) || !THPVariable_Check(f[1]) || !THPVariable_Check(f[2])) {
+            PyErr_SetString(PyExc_TypeError, "expected a SharedPrefix");
+            throw PythonError();
+        }
+        x.tables = (const int32_t *)typed_address(f[0], at::kInt, "int32");
+        x.lengths = (const int32_t *)typed_address(f[1], at::kInt, "int32");
+        x.starts = (const int32_t *)typed_address(f[2], at::kInt, "int32");
+        const at::Tensor &t = THPVariable_Unpack(f[0]);
+        if (t.dim() != 2 || THPVariable_Unpack(f[1]).numel() != t.size(0) || THPVariable_Unpack(f[2]).numel() != t.size(0) + 1) {
+            PyErr_SetString(PyExc_ValueError, "the tensors of a SharedPrefix do not belong together");
+            throw PythonError();
+        }
+        x.groups = t.size(0); x.table_width = t.size(1);
+        x.max_queries = integer(f[3]); x.max_length = integer(f[4]);
+    } catch (const PythonError &) {
+        Py_DECREF(five);
+        throw;
+    }
+    Py_DECREF(five);
+    return x;
+}
+
+float real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+    return (float)v;
+}
+
 template <class T> T argument(PyObject *o)
 {
+    if constexpr (std::is_same_v<T, dybit_heads>) return head_rows(o);
+    else if constexpr (std::is_same_v<T, dybit_kv_cache>) return kv_cache(o);
+    else if constexpr (std::is_same_v<T, dybit_kv_prefix>) return kv_prefix(o);
+    else if constexpr (std::is_same_v<T, float>) return real(o);
+    else if constexpr (std::is_same_v<T, const int64_t *>) return (T)typed_address(o, at::kLong, "int64");
+    else if constexpr (std::is_same_v<T, const int32_t *>) return (T)typed_address(o, at::kInt, "int32");
+    else
     if constexpr (std::is_same_v<T, dybit_fmt>) return format(o);
     else if constexpr (std::is_same_v<T, dybit_stream>) return stream_of(o);
     else if constexpr (std::is_pointer_v<T>) return (T)address(o);
@@ -178,6 +290,49 @@ PyObject *gemm(PyObject *self, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// dybit_kv_attention without its workspace, which comes from the allocator of the current stream and goes back to it after the call.
+PyObject *kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 13) {
+        PyErr_Format(PyExc_TypeError, "expected 13 arguments, got %zd", n);
+        return nullptr;
+    }
+    try {
+        const dybit_heads q = argument<dybit_heads>(args[0]);
+        const dybit_kv_cache cache = argument<dybit_kv_cache>(args[1]);
+        const int32_t *tables = argument<const int32_t *>(args[2]);
+        const int64_t width = integer(args[3]);
+        const int32_t *lengths = argument<const int32_t *>(args[4]), *starts = argument<const int32_t *>(args[5]);
+        const int64_t sequences = integer(args[6]), max_queries = integer(args[7]), max_length = integer(args[8]);
+        const int32_t causal = argument<int32_t>(args[9]);
+        const float scale = real(args[10]);
+        const dybit_kv_prefix prefix = kv_prefix(args[11]);
+        const dybit_heads out = head_rows(args[12]);
+        const size_t need = dybit_kv_attention_workspace_bytes(q, cache, width, sequences, max_queries, max_length, prefix);
+        const c10::DataPtr work = need ? c10::GetAllocator(c10::DeviceType::CUDA)->allocate(need) : c10::DataPtr();
+        dybit_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = dybit_kv_attention(q, cache, tables, width, lengths, starts, sequences, max_queries, max_length, causal, scale, prefix, out,
+                                (uint8_t *)work.get(), need, (dybit_stream)c10::hip::getCurrentHIPStream().stream());
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong((long)st);
+    } catch (const PythonError &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// empty_like(rows): an uninitialised contiguous tensor [tokens][heads][head_dim] of the same type.
+PyObject *empty_rows(PyObject *, PyObject *o)
+{
+    HANDLE_TH_ERRORS
+    if (!THPVariable_Check(o)) { PyErr_SetString(PyExc_TypeError, "expected a tensor"); return nullptr; }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return THPVariable_Wrap(at::empty(t.sizes(), t.options()));
+    END_HANDLE_TH_ERRORS
+}
+
 // empty(like, floats, *sizes): an uninitialised tensor of float32 (or, floats false, bytes) on the device of `like`.
 PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -216,6 +371,9 @@ PyMethodDef methods[] = {
     {"dybit_gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr}, DYBIT_ENTRY(dybit_gemm_ex), DYBIT_ENTRY(dybit_gemm_wb), DYBIT_ENTRY(dybit_gemm_wb_rc), DYBIT_ENTRY(dybit_gemm_pc),
     DYBIT_ENTRY(dybit_conv2d), DYBIT_ENTRY(dybit_conv2d_ex), DYBIT_ENTRY(dybit_conv2d_wb), DYBIT_ENTRY(dybit_conv2d_wb_rc), DYBIT_ENTRY(dybit_conv2d_pc),
     DYBIT_ENTRY(dybit_dwconv2d), DYBIT_ENTRY(dybit_dwconv2d_wb), DYBIT_ENTRY(dybit_group_conv2d), DYBIT_ENTRY(dybit_maxpool2d_codes),
+    DYBIT_ENTRY(dybit_head_norm_rope), DYBIT_ENTRY(dybit_head_norm_rope_bwd), DYBIT_ENTRY(dybit_kv_append), DYBIT_ENTRY(dybit_kv_copy_pages),
+    {"dybit_kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
+    {"empty_rows", (PyCFunction)empty_rows, METH_O, nullptr},
     {"dybit_packed_bytes", (PyCFunction)(void (*)(void))packed_bytes, METH_FASTCALL, nullptr},
     {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

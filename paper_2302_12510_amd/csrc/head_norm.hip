@@ -1,0 +1,335 @@
+// RMS norm of every query and key head with the rotation by the token's position, in one pass, and its gradient.
+//
+// A head is a list of D / 2 pairs: the rotated ones, then neighbours that pass unturned (a rotation with cos = 1, sin = 0).  A lane
+// holds V consecutive pairs, 2 V elements in two vector accesses, so a rotation never leaves its lane; the lanes of a head share
+// only the sum of squares (and, backward, the sum of h x).  A wave takes the heads of one token side by side: its rows of the
+// cosine and sine tables, and the weights, are read once for all of them.
+//   forward   n = x r w,  r = 1 / sqrt(mean x^2 + eps),  y = R n
+//   backward  g' = R^T g,  h = g' w,  dx = r (h - x r^2 mean(h x)),  dw = sum g' x r
+// Both are bound by memory: a head is read and written once (backward: read twice, written once).
+#include <hip/hip_runtime.h>
+
+#include "heads.h"
+
+namespace dybit {
+namespace headnorm {
+
+using heads::Pack;
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMostBlocks = 1024;                 // of the backward pass, whose partial sums of the weights' gradients are one row a block
+
+struct Args {
+    const void *x[2];                             // queries, keys
+    const void *g[2];
+    void *y[2];
+    const float *w[2];
+    int64_t xt[2], xh[2], gt[2], gh[2], yt[2], yh[2];       // strides by token and by head
+    int32_t heads[2];
+    const int64_t *positions;
+    const float *cos, *sin;
+    int64_t table_rows, tokens;
+    int32_t D, half;                              // half: rotated pairs
+    int32_t neighbours, parts, lanes;             // parts: waves per token; lanes per head (a power of two)
+    float eps;
+    int *err;
+    float *partial;                               // [blocks][2][D]
+};
+
+// Where the V pairs from p on lie: their first and their second elements as two runs, or interleaved in one run of 2 V.
+template <int V>
+struct Place {
+    int first, second;
+    bool woven;
+    __device__ __forceinline__ Place(int p, int half, int neighbours)
+    {
+        woven = neighbours || p >= half;
+        first = woven ? 2 * p : p;
+        second = woven ? 2 * p + V : p + half;
+    }
+};
+
+template <class T, int V>
+__device__ __forceinline__ void load_pairs(const T *row, const Place<V> &at, float (&a)[V], float (&b)[V])
+{
+    float u[V], v[V];
+    Pack<T, V>::load(row + at.first, u);
+    Pack<T, V>::load(row + at.second, v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float s = 2 * i < V ? u[(2 * i) % V] : v[(2 * i) % V], t = 2 * i + 1 < V ? u[(2 * i + 1) % V] : v[(2 * i + 1) % V];
+        a[i] = at.woven ? s : u[i];
+        b[i] = at.woven ? t : v[i];
+    }
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store_pairs(T *row, const Place<V> &at, const float (&a)[V], const float (&b)[V])
+{
+    float u[V], v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float s = i % 2 ? b[i / 2] : a[i / 2], t = (V + i) % 2 ? b[(V + i) / 2] : a[(V + i) / 2];
+        u[i] = at.woven ? s : a[i];
+        v[i] = at.woven ? t : b[i];
+    }
+    Pack<T, V>::store(row + at.first, u);
+    Pack<T, V>::store(row + at.second, v);
+}
+
+__device__ __forceinline__ float sum_over(float x, int lanes)
+{
+    for (int off = 1; off < lanes; off <<= 1) x += __shfl_xor(x, off);
+    return x;
+}
+
+// K: groups of V pairs per lane (1 except for heads that are wider than 64 lanes hold).
+template <class T, int V, int K, bool BACK>
+__global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int group = lane / p.lanes, groups = 64 / p.lanes, at = lane % p.lanes;
+    int pair[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) pair[k] = (at + k * p.lanes) * V;
+    float dw[2][K][2 * V];
+    if (BACK) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) dw[a][k][i] = 0.0f;
+    }
+    const int64_t units = p.tokens * p.parts;
+    for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < units; unit += (int64_t)gridDim.x * kWaves) {
+        const int64_t t = unit / p.parts;
+        const int part = (int)(unit - t * p.parts);
+        const int64_t position = p.positions[t];
+        const bool known = position >= 0 && position < p.table_rows;
+        float c[K][V], s[K][V];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) { c[k][i] = known ? 1.0f : __builtin_nanf(""); s[k][i] = 0.0f; }
+            if (known && pair[k] < p.half) {
+                Pack<float, V>::load(p.cos + position * p.half + pair[k], c[k]);
+                Pack<float, V>::load(p.sin + position * p.half + pair[k], s[k]);
+            }
+        }
+        if (!known && lane == 0) *p.err = DYBIT_ERR_INVALID_ARG;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            float wa[K][V], wb[K][V];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (p.heads[a] && pair[k] < p.D / 2) load_pairs<float, V>(p.w[a], Place<V>(pair[k], p.half, p.neighbours), wa[k], wb[k]);
+            // the waves of a token and the groups of a wave take turns at the heads; all lanes stay for the sums
+            for (int first = part * groups; first < p.heads[a]; first += p.parts * groups) {
+                const int h = first + group;
+                const bool in = h < p.heads[a];
+                float xa[K][V], xb[K][V], ga[K][V], gb[K][V];
+                float squares = 0.0f, dot = 0.0f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    if (in && pair[k] < p.D / 2) {
+                        const Place<V> place(pair[k], p.half, p.neighbours);
+                        load_pairs<T, V>((const T *)p.x[a] + t * p.xt[a] + h * p.xh[a], place, xa[k], xb[k]);
+                        if (BACK) load_pairs<T, V>((const T *)p.g[a] + t * p.gt[a] + h * p.gh[a], place, ga[k], gb[k]);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            squares += xa[k][i] * xa[k][i] + xb[k][i] * xb[k][i];
+                            if (BACK) {
+                                const float u = ga[k][i] * c[k][i] + gb[k][i] * s[k][i], v = gb[k][i] * c[k][i] - ga[k][i] * s[k][i];
+                                ga[k][i] = u;
+                                gb[k][i] = v;
+                                dot += u * wa[k][i] * xa[k][i] + v * wb[k][i] * xb[k][i];
+                            }
+                        }
+                    }
+                }
+                squares = sum_over(squares, p.lanes);
+                if (BACK) dot = sum_over(dot, p.lanes);
+                const float r = 1.0f / __builtin_sqrtf(squares / (float)p.D + p.eps);
+                const float pull = BACK ? dot / (float)p.D * r * r : 0.0f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    if (!in || pair[k] >= p.D / 2) continue;
+                    float ya[V], yb[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (BACK) {
+                            ya[i] = r * (ga[k][i] * wa[k][i] - xa[k][i] * pull);
+                            yb[i] = r * (gb[k][i] * wb[k][i] - xb[k][i] * pull);
+                            if (known) {
+                                dw[a][k][i] += ga[k][i] * (xa[k][i] * r);
+                                dw[a][k][V + i] += gb[k][i] * (xb[k][i] * r);
+                            }
+                        } else {
+                            const float u = xa[k][i] * r * wa[k][i], v = xb[k][i] * r * wb[k][i];
+                            ya[i] = u * c[k][i] - v * s[k][i];
+                            yb[i] = v * c[k][i] + u * s[k][i];
+                        }
+                    }
+                    store_pairs<T, V>((T *)p.y[a] + t * p.yt[a] + h * p.yh[a], Place<V>(pair[k], p.half, p.neighbours), ya, yb);
+                }
+            }
+        }
+    }
+    if constexpr (!BACK) return;
+    // the weights' gradients: over the groups of a wave, then over its block's waves, into the block's row
+    __shared__ float sums[kWaves][2][512];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) {
+                float x = dw[a][k][i];
+                for (int off = p.lanes; off < 64; off <<= 1) x += __shfl_xor(x, off);
+                dw[a][k][i] = x;
+            }
+            if (group == 0 && pair[k] < p.D / 2) {
+                const Place<V> place(pair[k], p.half, p.neighbours);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    sums[wave][a][place.woven ? 2 * (pair[k] + i) : place.first + i] = dw[a][k][i];
+                    sums[wave][a][place.woven ? 2 * (pair[k] + i) + 1 : place.second + i] = dw[a][k][V + i];
+                }
+            }
+        }
+    __syncthreads();
+    for (int j = threadIdx.x; j < 2 * p.D; j += kThreads) {
+        const int a = j >= p.D, d = j - a * p.D;
+        float x = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x += sums[w][a][d];
+        p.partial[(int64_t)blockIdx.x * 2 * p.D + j] = x;
+    }
+}
+
+// Sums the blocks' rows: a wave per 16 columns, four rows at a time, in an order that the number of blocks fixes.
+__global__ __launch_bounds__(64) void head_norm_sum_kernel(const float *partial, int blocks, int D, float *dwq, float *dwk)
+{
+    const int column = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    float x = 0.0f;
+    if (column < 2 * D)
+        for (int b = row; b < blocks; b += 4) x += partial[(int64_t)b * 2 * D + column];
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+    if (row == 0 && column < 2 * D) {
+        if (column < D) dwq[column] = x;
+        else if (dwk) dwk[column - D] = x;
+    }
+}
+
+int blocks_of(int64_t tokens) { return (int)(tokens < kMostBlocks * 2 ? (tokens + 1) / 2 : kMostBlocks); }
+
+template <class T, bool BACK>
+void launch(Args &p, int V, int blocks, hipStream_t st)
+{
+    int lanes = 1;
+    while (lanes < 64 && lanes * V < p.D / 2) lanes *= 2;
+    p.lanes = lanes;
+    const int groups = 64 / lanes, turns = (p.heads[0] + groups - 1) / groups;
+    if (BACK) {
+        p.parts = turns < 2 ? turns : 2;          // two tokens a block
+    } else {
+        p.parts = p.tokens >= 4096 ? 1 : turns;
+        blocks = (int)((p.tokens * p.parts + kWaves - 1) / kWaves);
+    }
+    if (p.parts < 1) p.parts = 1;
+    const dim3 grid((unsigned)blocks), block(kThreads);
+#define DYBIT_HN(V, K) hipLaunchKernelGGL((head_norm_kernel<T, V, K, BACK>), grid, block, 0, st, p)
+    if constexpr (sizeof(T) == 2)
+        if (V == 8) { DYBIT_HN(8, 1); return; }
+    if (V == 4) DYBIT_HN(4, 1);
+    else if (V == 2) DYBIT_HN(2, 1);
+    else DYBIT_HN(1, 4);
+#undef DYBIT_HN
+}
+
+bool aligned_floats(const float *p, int n) { return reinterpret_cast<uintptr_t>(p) % (4u * (unsigned)n) == 0; }
+
+dybit_status run(bool back, const dybit_heads *g, const dybit_heads *x, const dybit_heads *y, const float *const *w, const int64_t *positions,
+                 const float *cos_table, const float *sin_table, int64_t table_rows, int32_t rotary, int32_t neighbours, float eps,
+                 float *const *dw, float *workspace, hipStream_t st)
+{
+    const bool keys = x[1].heads > 0;
+    Args p{};
+    for (int a = 0; a < (keys ? 2 : 1); ++a)
+        for (const dybit_heads *h : {x + a, y + a, g ? g + a : x + a}) {
+            const dybit_status s = heads::check(*h);
+            if (s != DYBIT_OK) return s;
+            if (!heads::same_shape(*h, x[a]) || h->tokens != x[0].tokens || h->head_dim != x[0].head_dim || h->type != x[0].type) return DYBIT_ERR_INVALID_ARG;
+            if (!w[a]) return DYBIT_ERR_NULL;
+        }
+    if (!keys && (y[1].heads || (g && g[1].heads))) return DYBIT_ERR_INVALID_ARG;
+    const int D = x[0].head_dim;
+    if (D % 2 || D > 512 || rotary < 2 || rotary % 2 || rotary > D || table_rows < 0 || !(eps >= 0.0f) || (neighbours != 0 && neighbours != 1)) return DYBIT_ERR_INVALID_ARG;
+    if (back && (!dw[0] || (keys && !dw[1]) || !workspace)) return DYBIT_ERR_NULL;
+    if (back && !aligned16(workspace)) return DYBIT_ERR_ALIGNMENT;
+    if (x[0].tokens == 0 && !back) return DYBIT_OK;
+    if (x[0].tokens && (!positions || !cos_table || !sin_table)) return DYBIT_ERR_NULL;
+    int V = x[0].type == DYBIT_F32 ? 4 : 8;
+    auto fits = [&](int v) {
+        if ((D / 2) % v || (rotary / 2) % v || D / 2 > 64 * v || !aligned_floats(cos_table, v) || !aligned_floats(sin_table, v)) return false;
+        for (int a = 0; a < (keys ? 2 : 1); ++a)
+            if (!heads::aligned(x[a], v) || !heads::aligned(y[a], v) || (g && !heads::aligned(g[a], v)) || !aligned_floats(w[a], v)) return false;
+        return true;
+    };
+    while (V > 1 && !fits(V)) V /= 2;
+    for (int a = 0; a < (keys ? 2 : 1); ++a) {
+        p.x[a] = x[a].data; p.xt[a] = x[a].token_stride; p.xh[a] = x[a].head_stride;
+        p.y[a] = y[a].data; p.yt[a] = y[a].token_stride; p.yh[a] = y[a].head_stride;
+        if (g) { p.g[a] = g[a].data; p.gt[a] = g[a].token_stride; p.gh[a] = g[a].head_stride; }
+        p.w[a] = w[a];
+        p.heads[a] = x[a].heads;
+    }
+    p.positions = positions; p.cos = cos_table; p.sin = sin_table; p.table_rows = table_rows; p.tokens = x[0].tokens;
+    p.D = D; p.half = rotary / 2; p.neighbours = neighbours; p.eps = eps; p.partial = workspace;
+    p.err = async_error_word();
+    if (!p.err) return DYBIT_ERR_HIP;
+    const int blocks = back ? blocks_of(p.tokens) : 0;
+    if (p.tokens) {
+        switch (x[0].type) {
+            case DYBIT_F32: back ? launch<float, true>(p, V, blocks, st) : launch<float, false>(p, V, blocks, st); break;
+            case DYBIT_F16: back ? launch<_Float16, true>(p, V, blocks, st) : launch<_Float16, false>(p, V, blocks, st); break;
+            default: back ? launch<__bf16, true>(p, V, blocks, st) : launch<__bf16, false>(p, V, blocks, st); break;
+        }
+    }
+    if (back)
+        hipLaunchKernelGGL(head_norm_sum_kernel, dim3((unsigned)((2 * D + 15) / 16)), dim3(64), 0, st, workspace, blocks, D, dw[0], keys ? dw[1] : nullptr);
+    return launch_status();
+}
+
+}  // namespace headnorm
+}  // namespace dybit
+
+extern "C" dybit_status dybit_head_norm_rope(dybit_heads q, dybit_heads k, const float *q_weight, const float *k_weight,
+                                             const int64_t *positions, const float *cos_table, const float *sin_table, int64_t table_rows,
+                                             int32_t rotary, int32_t neighbours, float eps, dybit_heads q_out, dybit_heads k_out,
+                                             dybit_stream stream)
+{
+    const dybit_heads x[2] = {q, k}, y[2] = {q_out, k_out};
+    const float *w[2] = {q_weight, k_weight};
+    return dybit::headnorm::run(false, nullptr, x, y, w, positions, cos_table, sin_table, table_rows, rotary, neighbours, eps, nullptr, nullptr, (hipStream_t)stream);
+}
+
+extern "C" size_t dybit_head_norm_rope_bwd_workspace(int64_t tokens, int32_t heads, int32_t head_dim)
+{
+    if (tokens < 0 || heads < 0 || head_dim < 1) return 0;
+    return (size_t)(tokens ? dybit::headnorm::blocks_of(tokens) : 1) * 2 * (size_t)head_dim;
+}
+
+extern "C" dybit_status dybit_head_norm_rope_bwd(dybit_heads grad_q, dybit_heads grad_k, dybit_heads q, dybit_heads k,
+                                                 const float *q_weight, const float *k_weight, const int64_t *positions,
+                                                 const float *cos_table, const float *sin_table, int64_t table_rows,
+                                                 int32_t rotary, int32_t neighbours, float eps, dybit_heads dq, dybit_heads dk,
+                                                 float *q_weight_grad, float *k_weight_grad, float *workspace, dybit_stream stream)
+{
+    const dybit_heads g[2] = {grad_q, grad_k}, x[2] = {q, k}, y[2] = {dq, dk};
+    const float *w[2] = {q_weight, k_weight};
+    float *dw[2] = {q_weight_grad, k_weight_grad};
+    return dybit::headnorm::run(true, g, x, y, w, positions, cos_table, sin_table, table_rows, rotary, neighbours, eps, dw, workspace, (hipStream_t)stream);
+}

@@ -1,0 +1,288 @@
+// Attention over the cache of codes, one build per pair of code widths (DYBIT_KV_K, DYBIT_KV_V).
+//
+// S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_16x16x32_f16.  A row of the tile is one query head of one token; the heads that share
+// a key head, and neighbouring tokens, fill a tile of 16.  Every DyBit value of 4 and 8 bits is exact in fp16, so only the queries
+// and the probabilities are rounded:
+//   - a row of queries is multiplied by the power of two that brings its largest element to [2^14, 2^15) and rounded to fp16 (16-bit
+//     types: exact but for elements 2^-28 below the largest), or, from fp32, split into a sum of two halves (22 bits);
+//   - a probability times its value's scale is divided by a power of two over the largest such scale seen so far, times 2^14,
+//     and rounded to fp16 (fp32 outputs: two halves again).  The sum of the probabilities stays fp32 and unrounded.
+// The result of S^T (lane: one row, tokens 4 g + i) is the operand of O^T when its k slots are numbered that way, so probabilities
+// never change lanes.  Codes go from memory to registers to operands; no LDS in the loop.
+#include <hip/hip_runtime.h>
+
+#include "kv_attention_rows.h"
+
+#ifndef DYBIT_KV_K
+#define DYBIT_KV_K 8
+#endif
+#ifndef DYBIT_KV_V
+#define DYBIT_KV_V 8
+#endif
+
+namespace dybit {
+namespace kv {
+namespace {
+
+constexpr int KB = DYBIT_KV_K, VB = DYBIT_KV_V;
+constexpr int kThreads = 256, kWaves = 4;
+
+// 32 tokens of one key head as a lane holds them: codes of one token's run of keys and of eight tokens' values, and the scales.
+template <int D>
+struct Raw {
+    static constexpr int KW = D * KB / 128, VBYTES = D * VB / 128, VW = Values<VB, D / 16>::WORDS;
+    u32 k[2][KW];
+    u32 v[8][VW];
+    f32x4 sk[2], sv[2];
+};
+
+template <int D, int TERMS, int NT>
+__global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4;
+    const int head = blockIdx.x % p.kv_heads, seg = blockIdx.x / p.kv_heads;
+    const int64_t row0 = (int64_t)blockIdx.y * (16 * NT);
+    const int slot = blockIdx.z;
+    const Segment g = segment(p, seg);
+    if (g.odd && head == 0 && blockIdx.y == 0 && slot == 0 && threadIdx.x == 0) *p.err = DYBIT_ERR_INVALID_ARG;
+    if (row0 >= (int64_t)g.count * p.group) return;
+    // the keys of this workgroup: its chunk, as far as its last row sees
+    const int64_t last_row = row0 + 16 * NT - 1;
+    int last = (int)(last_row / p.group);
+    last = last < g.count ? last : g.count - 1;
+    const int lo = slot * p.chunk, most = visible(p, g, last);
+    const int hi = most - lo < p.chunk ? most : lo + p.chunk;
+    if (lo >= hi && p.part_out) return;
+
+    Rows<D, TERMS> r[NT];
+    State<D> st[NT];
+    int least = 0x7fffffff;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        load_rows<KB, D, TERMS>(p, g, head, row0 + 16 * t, lane, r[t]);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st[t].o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        st[t].m = -__builtin_inff();
+        st[t].l = 0.0f;
+        if (r[t].row >= 0) least = min(least, r[t].seen);
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
+    least = __builtin_amdgcn_readfirstlane(least);
+
+    // the pages of this wave's blocks of 16 tokens, one a lane: block j is step wave + 4 (j / 2), half j % 2
+    const int steps = (hi - lo + 31) >> 5;
+    const int32_t *table = p.tables + (int64_t)seg * p.table_width;
+    int page = -1;
+    {
+        const int token = lo + 32 * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
+        if (token < hi) {
+            page = table[token >> p.page_shift];
+            if (page < 0 || page >= p.pages) { page = -1; *p.err = DYBIT_ERR_INVALID_ARG; }
+        }
+    }
+    float vref = kFirstRef;
+    auto fetch = [&](Raw<D> &raw, int step) {
+        const int k = (step - wave) >> 2;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int id = max(__builtin_amdgcn_readlane(page, 2 * k + b), 0);
+            const int inside = (lo + 32 * step + 16 * b) & ((1 << p.page_shift) - 1);
+            const int64_t place = (((int64_t)id * p.kv_heads + head) << p.page_shift) + inside;
+            load_words<D * KB / 32>(p.k_codes + place * (D * KB / 8) + (lane & 15) * (D * KB / 8) + g4 * (D * KB / 32), raw.k[b]);
+            raw.sk[b] = *reinterpret_cast<const f32x4 *>(p.k_scales + place + 4 * g4);
+            raw.sv[b] = *reinterpret_cast<const f32x4 *>(p.v_scales + place + 4 * g4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                load_words<Raw<D>::VBYTES>(p.v_codes + place * (D * VB / 8) + (4 * g4 + i) * (D * VB / 8) + (lane & 15) * Raw<D>::VBYTES, raw.v[4 * b + i]);
+        }
+    };
+    auto go = [&](const Raw<D> &raw, int step) {
+        const int k = (step - wave) >> 2, token = lo + 32 * step;
+        int valid[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int left = hi - token - 16 * b;
+            valid[b] = __builtin_amdgcn_readlane(page, 2 * k + b) < 0 ? 0 : left < 16 ? left : 16;
+        }
+        const bool whole = valid[0] == 16 && valid[1] == 16 && token + 32 <= least;
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const f16x8 a = key_operand<KB>(raw.k[b], j);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < TERMS; ++e) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, r[t].q[e][j], s[t][b], 0, 0, 0);
+            }
+        }
+        // scales of the values; what lies past the end counts nothing, whatever it holds
+        float sv[8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sv[i] = whole || 4 * g4 + (i & 3) < valid[i >> 2] ? raw.sv[i >> 2][i & 3] : 0.0f;
+            top = fmaxf(top, sv[i]);
+        }
+        top = max_over_groups(top);
+        float shrink = 1.0f;
+        if (__builtin_amdgcn_readfirstlane(__float_as_uint(top)) > __float_as_uint(vref)) {
+            u32 e = (__float_as_uint(top) >> 23) + 1u;
+            e = e > 240u ? 240u : e;
+            const float ref = __uint_as_float(__builtin_amdgcn_readfirstlane(e) << 23);
+            shrink = vref / ref;
+            vref = ref;
+        }
+        const float up = kLargeP / vref;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sv[i] *= up;
+        f16x8 prob[NT][TERMS];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float x[8], mx = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = s[t][i >> 2][i & 3] * (raw.sk[i >> 2][i & 3] * r[t].factor);
+                if (!whole) {
+                    const int at = 4 * g4 + (i & 3);
+                    x[i] = at < valid[i >> 2] && token + 16 * (i >> 2) + at < r[t].seen ? x[i] : -__builtin_inff();
+                }
+                mx = fmaxf(mx, x[i]);
+            }
+            const float m = fmaxf(st[t].m, max_over_groups(mx));
+            const float base = m == -__builtin_inff() ? 0.0f : m;
+            const float keep = __builtin_amdgcn_exp2f(st[t].m - base);
+            st[t].m = m;
+            if (__any(keep * shrink != 1.0f)) {
+                st[t].l *= keep;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) st[t].o[j] *= keep * shrink;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(x[i] - base);
+                st[t].l += x[i];
+                x[i] *= sv[i];
+            }
+            u32 w[TERMS][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (TERMS == 2) split_pair(x[2 * i], x[2 * i + 1], w[0][i], w[1][i]);
+                else w[0][i] = round_pair(x[2 * i], x[2 * i + 1]);
+            }
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) prob[t][e] = operand(w[e][0], w[e][1], w[e][2], w[e][3]);
+        }
+        const Values<VB, D / 16> values(raw.v);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            const f16x8 a = values.dim(j);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][e], st[t].o[j], 0, 0, 0);
+        }
+    };
+    {
+        Raw<D> a, b;
+        int step = wave;
+        if (step < steps) fetch(a, step);
+        while (step < steps) {
+            if (step + kWaves < steps) fetch(b, step + kWaves);
+            go(a, step);
+            step += kWaves;
+            if (step >= steps) break;
+            if (step + kWaves < steps) fetch(a, step + kWaves);
+            go(b, step);
+            step += kWaves;
+        }
+    }
+
+    // join the four waves: 2 and 3 into 0 and 1, then 1 into 0
+    __shared__ float s_m[2][NT][16], s_l[2][NT][16], s_o[2][NT][D / 4][64];
+    const float back = vref / kLargeP * fold<VB>();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        st[t].l += __shfl_xor(st[t].l, 16);
+        st[t].l += __shfl_xor(st[t].l, 32);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st[t].o[j] *= back;
+    }
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (lane < 16) { s_m[wave - half][t][lane] = st[t].m; s_l[wave - half][t][lane] = st[t].l; }
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s_o[wave - half][t][4 * j + i][lane] = st[t].o[j][i];
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float m2 = s_m[wave][t][lane & 15], m = fmaxf(st[t].m, m2), base = m == -__builtin_inff() ? 0.0f : m;
+                const float a = __builtin_amdgcn_exp2f(st[t].m - base), b = __builtin_amdgcn_exp2f(m2 - base);
+                st[t].m = m;
+                st[t].l = st[t].l * a + s_l[wave][t][lane & 15] * b;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) st[t].o[j][i] = st[t].o[j][i] * a + s_o[wave][t][4 * j + i][lane] * b;
+            }
+        }
+        __syncthreads();
+    }
+    if (wave) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (r[t].row < 0) continue;
+        write_row<D>(p, r[t].row, slot, g4, st[t]);
+    }
+}
+
+template <int D, int TERMS>
+void launch_d(const Phase &p, const Plan &plan, int64_t segments, hipStream_t st)
+{
+    const dim3 grid((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots), block(kThreads);
+    if (D == 256 || plan.tiles16 == 1) hipLaunchKernelGGL((attention_kernel<D, TERMS, 1>), grid, block, 0, st, p);
+    else if constexpr (D < 256) hipLaunchKernelGGL((attention_kernel<D, TERMS, 2>), grid, block, 0, st, p);
+}
+
+void launch(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st)
+{
+    if (terms == 1) {
+        if (D == 64) launch_d<64, 1>(p, plan, segments, st);
+        else if (D == 128) launch_d<128, 1>(p, plan, segments, st);
+        else launch_d<256, 1>(p, plan, segments, st);
+    } else {
+        if (D == 64) launch_d<64, 2>(p, plan, segments, st);
+        else if (D == 128) launch_d<128, 2>(p, plan, segments, st);
+        else launch_d<256, 2>(p, plan, segments, st);
+    }
+}
+
+}  // namespace
+
+#if DYBIT_KV_K == 8 && DYBIT_KV_V == 8
+#define DYBIT_KV_LAUNCH launch_k8v8
+#elif DYBIT_KV_K == 8
+#define DYBIT_KV_LAUNCH launch_k8v4
+#elif DYBIT_KV_V == 8
+#define DYBIT_KV_LAUNCH launch_k4v8
+#else
+#define DYBIT_KV_LAUNCH launch_k4v4
+#endif
+void DYBIT_KV_LAUNCH(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st)
+{
+    launch(p, plan, D, terms, segments, st);
+}
+
+}  // namespace kv
+}  // namespace dybit

@@ -1,0 +1,264 @@
+// dybit_kv_attention: how a call is split, its launches, and the join of the parts that workgroups leave behind.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "kv_attention.h"
+
+namespace dybit {
+namespace kv {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+
+// ---- the plan ---------------------------------------------------------------------------------------------------------------------
+// Rows of a segment fill tiles of 16 a wave (32 where there are more than 16 rows); the tokens of a segment go to workgroups in chunks.
+// Chunks are as long as leaves kEnough workgroups, were all segments as long as the longest: short ones balance ragged batches and
+// fill the device, long ones leave fewer partial results (4 (D + 2) bytes a row and chunk, written and read back).
+constexpr int64_t kEnough = 1024;
+constexpr int32_t kShortest = 128, kLongest = 4096;       // a wave holds the pages of 64 blocks of 16 tokens, a quarter of a chunk
+
+Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int64_t cap)
+{
+    Plan p{};
+    p.tiles16 = max_rows > 16 && D < 256 ? 2 : 1;         // two tiles of 256 dims do not fit the registers
+    p.row_tiles = std::max<int64_t>(1, (max_rows + 16 * p.tiles16 - 1) / (16 * p.tiles16));
+    const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
+    p.chunk = kLongest;
+    while (p.chunk > kShortest && base * ((cap + p.chunk - 1) / p.chunk) < kEnough) p.chunk /= 2;
+    p.slots = std::max<int64_t>(1, (cap + p.chunk - 1) / p.chunk);
+    return p;
+}
+
+struct Split {
+    Plan own, prefix;
+    int64_t own_cap, prefix_cap, slots;                   // slots: 0 where workgroups write the results themselves
+};
+
+int64_t cap_of(const dybit_kv_cache &c, int64_t width, int64_t max_length)
+{
+    if (c.pages == 0) return 0;
+    const int64_t room = std::min<int64_t>(width * c.page_tokens, 0x7fffff00);
+    return max_length > 0 ? std::min(room, max_length) : room;
+}
+
+Split split_of(const dybit_heads &q, const dybit_kv_cache &c, int64_t width, int64_t sequences, int64_t max_queries, int64_t max_length,
+               const dybit_kv_prefix &prefix)
+{
+    Split s{};
+    const int group = q.heads / c.heads;
+    s.own_cap = cap_of(c, width, max_length);
+    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, s.own_cap);
+    if (prefix.groups) {
+        s.prefix_cap = cap_of(c, prefix.table_width, prefix.max_length);
+        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, s.prefix_cap);
+        s.slots = s.own.slots + s.prefix.slots;
+    } else {
+        s.slots = s.own.slots > 1 ? s.own.slots : 0;
+    }
+    return s;
+}
+
+dybit_status check_sizes(const dybit_heads &q, const dybit_kv_cache &c, int64_t width, int64_t sequences, int64_t max_queries, int64_t max_length,
+                         const dybit_kv_prefix &x)
+{
+    dybit_status st = check(c);
+    if (st != DYBIT_OK) return st;
+    st = heads::check(q);
+    if (st != DYBIT_OK) return st;
+    if (c.layers != 1 || q.head_dim != c.head_dim || q.heads < c.heads || q.heads % c.heads) return DYBIT_ERR_INVALID_ARG;
+    if (width < 0 || sequences < 0 || max_queries < 0 || max_length < 0 || x.groups < 0) return DYBIT_ERR_INVALID_ARG;
+    if (x.groups && (x.table_width < 0 || x.max_queries < 0 || x.max_length < 0)) return DYBIT_ERR_INVALID_ARG;
+    if (width > 0x7fffffff || x.table_width > 0x7fffffff) return DYBIT_ERR_INVALID_ARG;
+    if (sequences > 0xffff || sequences * c.heads > 1 << 24 || x.groups > sequences) return DYBIT_ERR_INVALID_ARG;
+    return DYBIT_OK;
+}
+
+// ---- the join ---------------------------------------------------------------------------------------------------------------------
+// Row by row: the parts' maxima and sums, then their outputs, weighted.  One wave a row, or WAVES of them where a row has many
+// parts.  Bound by reading the parts, which are still in the last-level cache.
+struct Join {
+    Phase own, prefix;
+    int32_t prefix_groups, own_slots, prefix_slots;
+};
+
+__device__ __forceinline__ void store_one(const Phase &p, int64_t at, float x)
+{
+    if (p.type == DYBIT_F32) ((float *)p.out)[at] = x;
+    else if (p.type == DYBIT_F16) ((_Float16 *)p.out)[at] = (_Float16)x;
+    else ((__bf16 *)p.out)[at] = (__bf16)x;
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(kThreads) void join_kernel(const Join p)
+{
+    constexpr int N = D / 64, ROWS = kWaves / WAVES;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = wave % WAVES;
+    const int heads_q = p.own.kv_heads * p.own.group;
+    const int64_t n = (int64_t)blockIdx.x * ROWS + wave / WAVES;
+    const int seq = blockIdx.y;
+    const Segment g = segment(p.own, seq);
+    const int i = (int)(n / heads_q), h = (int)(n - (int64_t)i * heads_q);
+    const bool real = i < g.count;
+    const int64_t row = real ? (g.first + i) * heads_q + h : 0;
+    int own = real ? (visible(p.own, g, i) + p.own.chunk - 1) / p.own.chunk : 0, before = 0;
+    if (real && p.prefix_groups) {
+        // the group that names this sequence
+        int a = 0, b = p.prefix_groups;
+        while (b - a > 1) {
+            const int mid = (a + b) >> 1;
+            if (p.prefix.members[mid] <= seq) a = mid; else b = mid;
+        }
+        if (p.prefix.members[a] <= seq && seq < p.prefix.members[a + 1]) {
+            const Segment whole = segment(p.prefix, a);
+            if (g.first >= whole.first && g.first + i < whole.first + whole.count) before = (whole.length + p.prefix.chunk - 1) / p.prefix.chunk;
+        }
+    }
+    // the row's slots one after the other: those of the prefix, then its own
+    const int count = before + own;
+    auto slot_of = [&](int j) { return (int64_t)(j < before ? j : p.prefix_slots + j - before); };
+    float m = -__builtin_inff(), l = 0.0f, x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = 0.0f;
+    for (int j0 = part * 64; j0 < count; j0 += WAVES * 64) {
+        const int j = j0 + lane;
+        float2 stat = float2{-__builtin_inff(), 0.0f};
+        if (j < count) stat = *reinterpret_cast<const float2 *>(p.own.part_stat + 2 * (slot_of(j) * p.own.rows + row));
+        float top = stat.x;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+        const float m2 = fmaxf(m, top), base = m2 == -__builtin_inff() ? 0.0f : m2;
+        const float keep = __builtin_amdgcn_exp2f(m - base), weight = __builtin_amdgcn_exp2f(stat.x - base);
+        float sum = stat.y * weight;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+        m = m2;
+        l = l * keep + sum;
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] *= keep;
+        const int end = count - j0 < 64 ? count - j0 : 64;
+        for (int s = 0; s < end; ++s) {
+            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s));
+            float y[N];
+            heads::Pack<float, N>::load(p.own.part_out + (slot_of(j0 + s) * p.own.rows + row) * D + N * lane, y);
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] += w * y[k];
+        }
+    }
+    if constexpr (WAVES > 1) {
+        __shared__ float s_m[kWaves], s_l[kWaves], s_x[kWaves][D];
+        if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
+        heads::Pack<float, N>::store(&s_x[wave][N * lane], x);
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            const float m2 = fmaxf(m, s_m[wave + w]), base = m2 == -__builtin_inff() ? 0.0f : m2;
+            const float a = __builtin_amdgcn_exp2f(m - base), b = __builtin_amdgcn_exp2f(s_m[wave + w] - base);
+            m = m2;
+            l = l * a + s_l[wave + w] * b;
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = x[k] * a + s_x[wave + w][N * lane + k] * b;
+        }
+    }
+    if (!real) return;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t at = (g.first + i) * p.own.out_token + h * p.own.out_head + N * lane;
+#pragma unroll
+    for (int k = 0; k < N; ++k) store_one(p.own, at + k, x[k] * inv);
+}
+
+void join(const Join &j, int D, int64_t max_queries, int64_t sequences, hipStream_t st)
+{
+    // four waves a row where it may have more parts than a wave's lanes ask for at once in a few turns
+    const bool many = j.own_slots + j.prefix_slots > 16;
+    const int64_t rows = max_queries * j.own.kv_heads * j.own.group, per_block = many ? 1 : kWaves;
+    const dim3 grid((unsigned)((rows + per_block - 1) / per_block), (unsigned)sequences), block(kThreads);
+#define DYBIT_JOIN(D) if (many) hipLaunchKernelGGL((join_kernel<D, 4>), grid, block, 0, st, j); \
+                      else hipLaunchKernelGGL((join_kernel<D, 1>), grid, block, 0, st, j)
+    if (D == 64) { DYBIT_JOIN(64); }
+    else if (D == 128) { DYBIT_JOIN(128); }
+    else { DYBIT_JOIN(256); }
+#undef DYBIT_JOIN
+}
+
+void launch(const Phase &p, const Plan &plan, const dybit_kv_cache &c, int64_t segments, hipStream_t st)
+{
+    const int terms = p.type == DYBIT_F32 ? 2 : 1;
+    switch (c.k_fmt.bits * 16 + c.v_fmt.bits) {
+        case 8 * 16 + 8: launch_k8v8(p, plan, c.head_dim, terms, segments, st); break;
+        case 8 * 16 + 4: launch_k8v4(p, plan, c.head_dim, terms, segments, st); break;
+        case 4 * 16 + 8: launch_k4v8(p, plan, c.head_dim, terms, segments, st); break;
+        default: launch_k4v4(p, plan, c.head_dim, terms, segments, st); break;
+    }
+}
+
+}  // namespace
+}  // namespace kv
+}  // namespace dybit
+
+extern "C" size_t dybit_kv_attention_workspace_bytes(dybit_heads q, dybit_kv_cache cache, int64_t table_width, int64_t sequences, int64_t max_queries,
+                                                     int64_t max_length, dybit_kv_prefix prefix)
+{
+    using namespace dybit;
+    if (kv::check_sizes(q, cache, table_width, sequences, max_queries, max_length, prefix) != DYBIT_OK) return 0;
+    if (q.tokens == 0 || sequences == 0) return 0;
+    const kv::Split s = kv::split_of(q, cache, table_width, sequences, max_queries, max_length, prefix);
+    return (size_t)s.slots * (size_t)q.tokens * (size_t)q.heads * (size_t)(q.head_dim + 2) * 4;
+}
+
+extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, const int32_t *tables, int64_t table_width, const int32_t *lengths,
+                                           const int32_t *starts, int64_t sequences, int64_t max_queries, int64_t max_length, int32_t causal,
+                                           float scale, dybit_kv_prefix prefix, dybit_heads out, uint8_t *workspace, size_t workspace_bytes,
+                                           dybit_stream stream)
+{
+    using namespace dybit;
+    dybit_status st = kv::check_sizes(q, cache, table_width, sequences, max_queries, max_length, prefix);
+    if (st != DYBIT_OK) return st;
+    st = heads::check(out);
+    if (st != DYBIT_OK) return st;
+    if (!heads::same_shape(q, out) || (causal != 0 && causal != 1) || !std::isfinite(scale)) return DYBIT_ERR_INVALID_ARG;
+    if (q.tokens == 0 || sequences == 0 || max_queries == 0) return DYBIT_OK;
+    if (!lengths || (!tables && table_width)) return DYBIT_ERR_NULL;
+    if (prefix.groups && ((!prefix.tables && prefix.table_width) || !prefix.lengths || !prefix.starts)) return DYBIT_ERR_NULL;
+    const kv::Split s = kv::split_of(q, cache, table_width, sequences, max_queries, max_length, prefix);
+    // grids: y (row tiles; sequences in the join) and z (chunks) stay under 2^16
+    if (s.own.row_tiles > 65535 || s.own.slots > 65535 || s.prefix.row_tiles > 65535 || s.prefix.slots > 65535) return DYBIT_ERR_INVALID_ARG;
+    const int64_t rows = q.tokens * q.heads;
+    const size_t need = (size_t)s.slots * (size_t)rows * (size_t)(q.head_dim + 2) * 4;
+    if (need > workspace_bytes) return DYBIT_ERR_INVALID_ARG;
+    if (need && !workspace) return DYBIT_ERR_NULL;
+    if (need && !aligned16(workspace)) return DYBIT_ERR_ALIGNMENT;
+    hipStream_t hs = (hipStream_t)stream;
+    kv::Phase p{};
+    p.q = q.data; p.q_token = q.token_stride; p.q_head = q.head_stride;
+    p.out = out.data; p.out_token = out.token_stride; p.out_head = out.head_stride;
+    p.type = q.type; p.q_vectors = heads::aligned(q, 8); p.out_vectors = heads::aligned(out, 8);
+    p.k_codes = cache.k_codes; p.k_scales = cache.k_scales; p.v_codes = cache.v_codes; p.v_scales = cache.v_scales;
+    p.pages = cache.pages;
+    p.kv_heads = cache.heads; p.group = q.heads / cache.heads; p.page_shift = kv::log2_of(cache.page_tokens);
+    p.starts = starts; p.tokens = q.tokens; p.sequences = sequences;
+    p.scale = scale * 1.44269504088896340736f;
+    p.part_out = need ? (float *)workspace : nullptr;
+    p.part_stat = need ? (float *)workspace + (size_t)s.slots * (size_t)rows * (size_t)q.head_dim : nullptr;
+    p.rows = rows;
+    p.err = async_error_word();
+    if (!p.err) return DYBIT_ERR_HIP;
+    kv::Join j{};
+    j.own = p;
+    j.own.tables = tables; j.own.lengths = lengths; j.own.table_width = table_width; j.own.max_queries = max_queries; j.own.cap = s.own_cap;
+    j.own.causal = causal; j.own.chunk = s.own.chunk; j.own.slot0 = prefix.groups ? s.prefix.slots : 0;
+    j.own_slots = (int32_t)s.own.slots;
+    if (prefix.groups) {
+        j.prefix = p;
+        j.prefix.tables = prefix.tables; j.prefix.lengths = prefix.lengths; j.prefix.members = prefix.starts;
+        j.prefix.table_width = prefix.table_width; j.prefix.max_queries = prefix.max_queries; j.prefix.cap = s.prefix_cap;
+        j.prefix.causal = 0; j.prefix.chunk = s.prefix.chunk; j.prefix.slot0 = 0;
+        j.prefix_groups = (int32_t)prefix.groups; j.prefix_slots = (int32_t)s.prefix.slots;
+        kv::launch(j.prefix, s.prefix, cache, prefix.groups, hs);
+    }
+    kv::launch(j.own, s.own, cache, sequences, hs);
+    if (need) kv::join(j, cache.head_dim, max_queries, sequences, hs);
+    return launch_status();
+}

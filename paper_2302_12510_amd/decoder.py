@@ -1,0 +1,137 @@
+"""A small decoder over the library's entry points: coded weights and activations in the products, a paged cache of coded keys and
+values, norms of heads with rotation, attention with a shared prefix.  Random weights; run as a program, it answers from one prompt
+in several branches:
+
+    python -m paper_2302_12510_amd.decoder
+
+Every product takes 8-bit codes of its input and 4- or 8-bit codes of its weights, both with a scale per row, so that what a token
+gives does not depend on the tokens beside it.  Torch adds residuals, normalises rows and looks embeddings up.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+
+import torch
+
+from . import binding as B
+from .kv_cache import PagedCache
+
+ACT = (8, True)
+
+
+@dataclass(frozen=True)
+class Config:
+    layers: int = 4
+    hidden: int = 512
+    heads: int = 8
+    kv_heads: int = 2
+    head_dim: int = 64
+    wide: int = 1024
+    vocabulary: int = 1000
+    w_bits: int = 4
+    k_bits: int = 8
+    v_bits: int = 4
+    page_tokens: int = 16
+    pages: int = 256
+    positions: int = 4096
+    eps: float = 1e-6
+
+
+class Linear:
+    def __init__(self, w: torch.Tensor, bits: int):
+        self.rows, self.cols = w.shape
+        self.fmt = (bits, True)
+        self.scales, self.codes = B.dybit_quantize_rows(w.contiguous(), bits, True)
+        self.one = torch.ones(1, device=w.device)
+
+    def __call__(self, x: torch.Tensor, relu: bool = False) -> torch.Tensor:
+        s, codes = B.dybit_quantize_rows(x.contiguous(), *ACT)
+        y, _ = B.dybit_gemm_pc(x.shape[0], self.rows, self.cols, codes, ACT, self.one, self.codes, self.fmt, self.scales, relu=relu)
+        return y.mul_(s.unsqueeze(1))                     # a positive factor: behind the ReLU as before it
+
+
+class Decoder:
+    def __init__(self, config: Config, seed: int = 0, device="cuda"):
+        c = self.config = config
+        g = torch.Generator(device=device).manual_seed(seed)
+        normal = lambda *n, s: torch.randn(*n, generator=g, device=device) * s  # noqa: E731
+        self.embedding = normal(c.vocabulary, c.hidden, s=1.0)
+        q, kv = c.heads * c.head_dim, c.kv_heads * c.head_dim
+        self.layers = [{
+            "qkv": Linear(normal(q + 2 * kv, c.hidden, s=c.hidden ** -0.5), c.w_bits),
+            "out": Linear(normal(c.hidden, q, s=q ** -0.5), c.w_bits),
+            "up": Linear(normal(c.wide, c.hidden, s=c.hidden ** -0.5), c.w_bits),
+            "down": Linear(normal(c.hidden, c.wide, s=c.wide ** -0.5), c.w_bits),
+            "q_norm": 1 + normal(c.head_dim, s=0.1), "k_norm": 1 + normal(c.head_dim, s=0.1),
+        } for _ in range(c.layers)]
+        self.head = Linear(normal(c.vocabulary, c.hidden, s=c.hidden ** -0.5), 8)
+        angle = torch.arange(c.positions, device=device, dtype=torch.float64)[:, None] * \
+            10000.0 ** (-torch.arange(0, c.head_dim, 2, device=device, dtype=torch.float64) / c.head_dim)
+        self.cos, self.sin = angle.cos().float(), angle.sin().float()
+        self.store = PagedCache(c.layers, c.pages, c.kv_heads, c.page_tokens, c.head_dim, c.k_bits, c.v_bits, device)
+
+    def _norm(self, x):
+        return x * torch.rsqrt((x * x).mean(-1, keepdim=True) + self.config.eps)
+
+    def step(self, seqs, tokens, prefix=None) -> torch.Tensor:
+        """Logits after the last of the new tokens of every sequence: tokens[i] (a list, at least one) goes behind seqs[i].
+        prefix: (sequence, that of all of them in front of their own tokens), or None."""
+        c, store = self.config, self.store
+        counts = [len(t) for t in tokens]
+        before = store.tokens(prefix) if prefix is not None else 0
+        at = [before + store.tokens(s) for s in seqs]
+        device = self.embedding.device
+        positions = torch.cat([torch.arange(a, a + n) for a, n in zip(at, counts)]).to(device)
+        slots = torch.cat([torch.from_numpy(store.extend(s, n)) for s, n in zip(seqs, counts)]).to(device)
+        tables, lengths = store.device_tables(seqs)
+        starts = torch.tensor([sum(counts[:i]) for i in range(len(counts) + 1)], dtype=torch.int32, device=device)
+        shared = None
+        if prefix is not None:
+            shared = B.SharedPrefix(*store.device_tables([prefix]), torch.tensor([0, len(seqs)], dtype=torch.int32, device=device), sum(counts))
+        x = self.embedding[torch.tensor([t for ts in tokens for t in ts], device=device)]
+        T = x.shape[0]
+        for i, layer in enumerate(self.layers):
+            qkv = layer["qkv"](self._norm(x)).view(T, c.heads + 2 * c.kv_heads, c.head_dim)
+            q, k, v = qkv[:, :c.heads], qkv[:, c.heads:c.heads + c.kv_heads], qkv[:, c.heads + c.kv_heads:]
+            B.dybit_head_norm_rope(q, k, layer["q_norm"], layer["k_norm"], positions, self.cos, self.sin, c.eps, out=(q, k))
+            B.dybit_kv_append(k, v, slots, store.layer(i))
+            y = B.dybit_kv_attention(q, store.layer(i), tables, lengths, starts, max_queries=max(counts), prefix=shared)
+            x = x + layer["out"](y.view(T, -1))
+            x = x + layer["down"](layer["up"](self._norm(x), relu=True))
+        return self.head(self._norm(x[starts[1:].long() - 1]))
+
+
+def generate(model: Decoder, prompt, branches: int = 4, length: int = 24, keep: int = 2, seed: int = 0):
+    """Answers to one prompt: half of them behind the prompt as a shared prefix, half as forks of it; in the middle some branches are
+    dropped and the pool is compacted.  Returns the tokens of the branches that are left."""
+    store, g = model.store, torch.Generator().manual_seed(seed)
+
+    def pick(logits):
+        return torch.multinomial(torch.softmax(logits.cpu() / 2, -1), 1, generator=g).view(-1).tolist()
+    store.add("prompt")
+    logits = model.step(["prompt"], [prompt])
+    forks, tails = [("fork", i) for i in range(branches)], [("tail", i) for i in range(branches)]
+    store.fork("prompt", forks)
+    for s in tails:
+        store.add(s)
+    answers = {s: [t] for s, t in zip(forks + tails, pick(logits.expand(2 * branches, -1)))}
+    for n in range(length):
+        if n == length // 2:
+            for s in forks[keep:] + tails[keep:]:
+                store.free(s)
+                del answers[s]
+            forks, tails = forks[:keep], tails[:keep]
+            store.compact()
+        for seqs, prefix in ((forks, None), (tails, "prompt")):
+            logits = model.step(seqs, [answers[s][-1:] for s in seqs], prefix)
+            for s, t in zip(seqs, pick(logits)):
+                answers[s].append(t)
+    return answers
+
+
+if __name__ == "__main__":
+    model = Decoder(Config())
+    rng = torch.Generator().manual_seed(1)
+    for branch, answer in generate(model, torch.randint(0, model.config.vocabulary, (100,), generator=rng).tolist()).items():
+        print(*branch, answer)
+    print("pages in use:", int((model.store.owners > 0).sum()), "async error:", B.dybit_get_last_async_error())

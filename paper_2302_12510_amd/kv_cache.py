@@ -1,0 +1,149 @@
+"""Pages of the key/value cache: which sequence owns which, and the tensors behind them.
+
+`PagePool` is the bookkeeping, on the host: a sequence is a list of pages and a number of tokens; full pages may belong to
+several sequences, a page that is still being filled to one.  `PagedCache` adds the tensors of all layers and runs the copies
+that forking and compacting need, one launch each.
+"""
+from __future__ import annotations
+
+import heapq
+
+import numpy as np
+import torch
+
+from . import binding as B
+
+
+class PoolFull(RuntimeError):
+    """No free page is left; nothing was changed."""
+
+
+class PagePool:
+    def __init__(self, pages: int, page_tokens: int):
+        if pages < 0 or page_tokens < 1:
+            raise ValueError("expected a number of pages and of tokens in a page")
+        self.page_tokens = page_tokens
+        self.owners = np.zeros(pages, np.int32)                   # sequences that a page belongs to
+        self._free = list(range(pages))                           # a heap: low pages first, so that pools stay compact
+        self._pages: dict[object, list[int]] = {}
+        self._tokens: dict[object, int] = {}
+
+    def __contains__(self, seq) -> bool:
+        return seq in self._pages
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def tokens(self, seq) -> int:
+        return self._tokens[seq]
+
+    def pages(self, seq) -> tuple[int, ...]:
+        return tuple(self._pages[seq])
+
+    def _take(self, n: int) -> list[int]:
+        if n > len(self._free):
+            raise PoolFull(f"{n} pages wanted, {len(self._free)} free")
+        got = [heapq.heappop(self._free) for _ in range(n)]
+        self.owners[got] = 1
+        return got
+
+    def add(self, seq) -> None:
+        """A sequence without tokens."""
+        if seq in self._pages:
+            raise KeyError(f"sequence {seq!r} is there already")
+        self._pages[seq], self._tokens[seq] = [], 0
+
+    def extend(self, seq, n: int = 1) -> np.ndarray:
+        """Places (int64, page * page_tokens + place) of the next n tokens of a sequence."""
+        if n < 0:
+            raise ValueError("expected a number of tokens")
+        pages, at = self._pages[seq], self._tokens[seq]
+        pages += self._take(-(-(at + n) // self.page_tokens) - len(pages))
+        self._tokens[seq] = at + n
+        t = np.arange(at, at + n, dtype=np.int64)
+        return np.asarray(pages, np.int64)[t // self.page_tokens] * self.page_tokens + t % self.page_tokens if n else t
+
+    def fork(self, parent, children) -> list[tuple[int, int]]:
+        """Sequences with the tokens of `parent`: full pages are shared, the page in the middle of which it is is copied.  Returns
+        the copies to make, (from, to), before anything else writes to the pool."""
+        children = list(children)
+        if len(set(children)) != len(children) or any(c in self._pages for c in children):
+            raise KeyError("a sequence to fork into is there already")
+        pages, n = self._pages[parent], self._tokens[parent]
+        full = n // self.page_tokens
+        own = self._take(len(children) if n % self.page_tokens else 0)
+        for i, child in enumerate(children):
+            self.owners[pages[:full]] += 1
+            self._pages[child] = pages[:full] + own[i:i + 1]
+            self._tokens[child] = n
+        return [(pages[full], to) for to in own]
+
+    def free(self, seq) -> None:
+        """Forgets a sequence; pages that no other one has are free again."""
+        for p in self._pages.pop(seq):
+            self.owners[p] -= 1
+            if not self.owners[p]:
+                heapq.heappush(self._free, p)
+        del self._tokens[seq]
+
+    def compact(self) -> list[tuple[int, int]]:
+        """Moves pages so that those in use are the first ones of the pool.  Returns the copies to make, (from, to): no page of
+        either list is in the other.  Page numbers handed out before are void."""
+        used = int(np.count_nonzero(self.owners))
+        src = [int(p) for p in np.flatnonzero(self.owners[used:]) + used]
+        dst = [int(p) for p in np.flatnonzero(self.owners[:used] == 0)]
+        move = dict(zip(src, dst))
+        for pages in self._pages.values():
+            pages[:] = [move.get(p, p) for p in pages]
+        self.owners[dst] = self.owners[src]
+        self.owners[src] = 0
+        self._free = list(range(used, len(self.owners)))
+        return list(zip(src, dst))
+
+    def tables(self, seqs, width: int | None = None) -> tuple[np.ndarray, np.ndarray]:
+        """(page numbers int32 [sequences][width], -1 behind a sequence's last page; tokens int32 [sequences])."""
+        lists = [self._pages[s] for s in seqs]
+        need = max((len(p) for p in lists), default=0)
+        width = max(1, need) if width is None else width
+        if width < need:
+            raise ValueError(f"a sequence has {need} pages, the table {width}")
+        table = np.full((len(lists), width), -1, np.int32)
+        for row, p in zip(table, lists):
+            row[:len(p)] = p
+        return table, np.array([self._tokens[s] for s in seqs], np.int32)
+
+
+class PagedCache(PagePool):
+    """A pool and the tensors of all layers behind it."""
+
+    def __init__(self, layers: int, pages: int, heads: int, page_tokens: int, head_dim: int, k_bits: int = 8, v_bits: int = 8, device="cuda"):
+        super().__init__(pages, page_tokens)
+        new = lambda *last, dtype: torch.empty(layers, pages, heads, page_tokens, *last, dtype=dtype, device=device)  # noqa: E731
+        self.cache = B.KVCache(new(head_dim * k_bits // 8, dtype=torch.uint8), new(dtype=torch.float32),
+                               new(head_dim * v_bits // 8, dtype=torch.uint8), new(dtype=torch.float32), k_bits, v_bits)
+        self._layers = [self.cache.layer(i) for i in range(layers)]
+
+    def layer(self, i: int) -> B.KVCache:
+        return self._layers[i]
+
+    def _copy(self, pairs) -> None:
+        if pairs:
+            moves = torch.tensor(pairs, dtype=torch.int32).t().contiguous().to(self.cache.k_codes.device)
+            B.dybit_kv_copy_pages(self.cache, moves[0], moves[1])
+
+    def fork(self, parent, children) -> list[tuple[int, int]]:
+        pairs = super().fork(parent, children)
+        self._copy(pairs)
+        return pairs
+
+    def compact(self) -> list[tuple[int, int]]:
+        pairs = super().compact()
+        self._copy(pairs)
+        return pairs
+
+    def device_slots(self, places) -> torch.Tensor:
+        return torch.from_numpy(np.ascontiguousarray(places, dtype=np.int64)).to(self.cache.k_codes.device)
+
+    def device_tables(self, seqs, width: int | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+        return tuple(torch.from_numpy(a).to(self.cache.k_codes.device) for a in self.tables(seqs, width))
