@@ -106,6 +106,10 @@ SOURCES = [
     ("kv_attention.hip", "kv_attention_k8v4", ["-DDYBIT_KV_K=8", "-DDYBIT_KV_V=4"]),
     ("kv_attention.hip", "kv_attention_k4v8", ["-DDYBIT_KV_K=4", "-DDYBIT_KV_V=8"]),
     ("kv_attention.hip", "kv_attention_k4v4", ["-DDYBIT_KV_K=4", "-DDYBIT_KV_V=4"]),
+    ("kv_attention_wide.hip", "kv_attention_wide_k8v8", ["-DDYBIT_KV_K=8", "-DDYBIT_KV_V=8"]),
+    ("kv_attention_wide.hip", "kv_attention_wide_k8v4", ["-DDYBIT_KV_K=8", "-DDYBIT_KV_V=4"]),
+    ("kv_attention_wide.hip", "kv_attention_wide_k4v8", ["-DDYBIT_KV_K=4", "-DDYBIT_KV_V=8"]),
+    ("kv_attention_wide.hip", "kv_attention_wide_k4v4", ["-DDYBIT_KV_K=4", "-DDYBIT_KV_V=4"]),
     ("diag.hip", "diag", []),
 ]
 FLAGS = ["--offload-arch=gfx950", "--offload-compress", "-O3", "-fPIC", "-std=c++17",

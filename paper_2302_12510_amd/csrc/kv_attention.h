@@ -69,7 +69,8 @@ __device__ __forceinline__ int visible(const Phase &p, const Segment &g, int i)
 
 // How a phase is run: decided on the host from sizes alone.
 struct Plan {
-    int32_t tiles16;                                   // 16-row tiles of a wave: 1 or 2
+    bool wide;                                         // kv_attention_wide.hip, else kv_attention.hip
+    int32_t tiles16;                                   // 16-row tiles of a wave of the latter: 1 or 2
     int32_t chunk;
     int64_t row_tiles, slots;
 };
@@ -78,6 +79,11 @@ void launch_k8v8(const Phase &p, const Plan &plan, int D, int terms, int64_t seg
 void launch_k8v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
 void launch_k4v8(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
 void launch_k4v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
+void launch_wide_k8v8(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
+void launch_wide_k8v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
+void launch_wide_k4v8(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
+void launch_wide_k4v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
+constexpr int kWideRows = 128;                         // rows of a workgroup of the wide kernel
 
 }  // namespace kv
 }  // namespace dybit

@@ -13,20 +13,23 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 
 // ---- the plan ---------------------------------------------------------------------------------------------------------------------
-// Rows of a segment fill tiles of 16 a wave (32 where there are more than 16 rows); the tokens of a segment go to workgroups in chunks.
-// Chunks are as long as leaves kEnough workgroups, were all segments as long as the longest: short ones balance ragged batches and
-// fill the device, long ones leave fewer partial results (4 (D + 2) bytes a row and chunk, written and read back).
-constexpr int64_t kEnough = 1024;
+// Up to 32 rows of a segment are one or two tiles of a wave, whose waves share the keys of a chunk out; more go to the wide kernel,
+// whose waves share the rows out.  The tokens of a segment go to workgroups in chunks, as long ones as leave kEnough workgroups, were
+// all segments as long as the longest: short ones balance ragged batches and fill the device, long ones leave fewer partial
+// results (4 (D + 2) bytes a row and chunk, written and read back).
+constexpr int64_t kEnough = 1024, kEnoughWide = 512;
 constexpr int32_t kShortest = 128, kLongest = 4096;       // a wave holds the pages of 64 blocks of 16 tokens, a quarter of a chunk
 
 Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int64_t cap)
 {
     Plan p{};
+    p.wide = max_rows > 32;
     p.tiles16 = max_rows > 16 && D < 256 ? 2 : 1;         // two tiles of 256 dims do not fit the registers
-    p.row_tiles = std::max<int64_t>(1, (max_rows + 16 * p.tiles16 - 1) / (16 * p.tiles16));
-    const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
-    p.chunk = kLongest;
-    while (p.chunk > kShortest && base * ((cap + p.chunk - 1) / p.chunk) < kEnough) p.chunk /= 2;
+    const int64_t rows = p.wide ? kWideRows : 16 * p.tiles16;
+    p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
+    const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles), enough = p.wide ? kEnoughWide : kEnough;
+    p.chunk = p.wide ? 1 << 30 : kLongest;
+    while (p.chunk > kShortest && base * std::max<int64_t>(1, (cap + p.chunk - 1) / p.chunk) < enough) p.chunk /= 2;
     p.slots = std::max<int64_t>(1, (cap + p.chunk - 1) / p.chunk);
     return p;
 }
@@ -186,12 +189,10 @@ void join(const Join &j, int D, int64_t max_queries, int64_t sequences, hipStrea
 void launch(const Phase &p, const Plan &plan, const dybit_kv_cache &c, int64_t segments, hipStream_t st)
 {
     const int terms = p.type == DYBIT_F32 ? 2 : 1;
-    switch (c.k_fmt.bits * 16 + c.v_fmt.bits) {
-        case 8 * 16 + 8: launch_k8v8(p, plan, c.head_dim, terms, segments, st); break;
-        case 8 * 16 + 4: launch_k8v4(p, plan, c.head_dim, terms, segments, st); break;
-        case 4 * 16 + 8: launch_k4v8(p, plan, c.head_dim, terms, segments, st); break;
-        default: launch_k4v4(p, plan, c.head_dim, terms, segments, st); break;
-    }
+    const int widths = c.k_fmt.bits * 16 + c.v_fmt.bits;
+    const auto run = plan.wide ? (widths == 8 * 16 + 8 ? launch_wide_k8v8 : widths == 8 * 16 + 4 ? launch_wide_k8v4 : widths == 4 * 16 + 8 ? launch_wide_k4v8 : launch_wide_k4v4)
+                               : (widths == 8 * 16 + 8 ? launch_k8v8 : widths == 8 * 16 + 4 ? launch_k8v4 : widths == 4 * 16 + 8 ? launch_k4v8 : launch_k4v4);
+    run(p, plan, c.head_dim, terms, segments, st);
 }
 
 }  // namespace
