@@ -208,19 +208,31 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
     }
 }
 
-// Sums the blocks' rows: a wave per 16 columns, four rows at a time, in an order that the number of blocks fixes.
-__global__ __launch_bounds__(64) void head_norm_sum_kernel(const float *partial, int blocks, int D, float *dwq, float *dwk)
+// Sums the blocks' rows: a workgroup per 16 columns, 64 rows at a time, in an order that the number of blocks fixes.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void head_norm_sum_kernel(const float *partial, int blocks, int D, float *dwq, float *dwk)
 {
-    const int column = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    constexpr int ROWS = kSumThreads / 16, TURNS = kMostBlocks / ROWS;
+    const int at = threadIdx.x & 15, column = blockIdx.x * 16 + at, row = threadIdx.x >> 4;
     float x = 0.0f;
-    if (column < 2 * D)
-        for (int b = row; b < blocks; b += 4) x += partial[(int64_t)b * 2 * D + column];
+    if (column < 2 * D) {
+        float y[TURNS];                                    // all requested before the first is added
+#pragma unroll
+        for (int k = 0; k < TURNS; ++k) y[k] = row + k * ROWS < blocks ? partial[(int64_t)(row + k * ROWS) * 2 * D + column] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < TURNS; ++k) x += y[k];
+    }
     x += __shfl_xor(x, 16);
     x += __shfl_xor(x, 32);
-    if (row == 0 && column < 2 * D) {
-        if (column < D) dwq[column] = x;
-        else if (dwk) dwk[column - D] = x;
-    }
+    __shared__ float sums[kSumThreads / 64][16];
+    if ((threadIdx.x & 63) < 16) sums[threadIdx.x >> 6][at] = x;
+    __syncthreads();
+    if (threadIdx.x >= 16 || column >= 2 * D) return;
+    x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kSumThreads / 64; ++w) x += sums[w][at];
+    if (column < D) dwq[column] = x;
+    else if (dwk) dwk[column - D] = x;
 }
 
 int blocks_of(int64_t tokens) { return (int)(tokens < kMostBlocks * 2 ? (tokens + 1) / 2 : kMostBlocks); }
@@ -299,7 +311,7 @@ dybit_status run(bool back, const dybit_heads *g, const dybit_heads *x, const dy
         }
     }
     if (back)
-        hipLaunchKernelGGL(head_norm_sum_kernel, dim3((unsigned)((2 * D + 15) / 16)), dim3(64), 0, st, workspace, blocks, D, dw[0], keys ? dw[1] : nullptr);
+        hipLaunchKernelGGL(head_norm_sum_kernel, dim3((unsigned)((2 * D + 15) / 16)), dim3(kSumThreads), 0, st, workspace, blocks, D, dw[0], keys ? dw[1] : nullptr);
     return launch_status();
 }
 

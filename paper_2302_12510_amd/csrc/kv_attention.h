@@ -20,8 +20,8 @@ struct Phase {
     int64_t max_queries, cap;                          // cap: most tokens of a segment that are looked at
     int32_t causal, chunk;                             // chunk: tokens of a segment that one workgroup goes through
     float scale;                                       // times log2(e)
-    float *part_out, *part_stat;                       // partial results [slot][token][query head][D], (maximum, sum); NULL: write out
-    int64_t slot0, rows;                               // first slot of the phase; tokens * query heads
+    float *part_out, *part_stat;                       // partial results [token][query head][slot][D], (maximum, sum); NULL: write out
+    int64_t slot0, slots;                              // first slot of the phase; slots of a row
     int *err;
 };
 

@@ -71,7 +71,7 @@ dybit_status check_sizes(const dybit_heads &q, const dybit_kv_cache &c, int64_t 
     st = heads::check(q);
     if (st != DYBIT_OK) return st;
     if (c.layers != 1 || q.head_dim != c.head_dim || q.heads < c.heads || q.heads % c.heads) return DYBIT_ERR_INVALID_ARG;
-    if (width < 0 || sequences < 0 || max_queries < 0 || max_length < 0 || x.groups < 0) return DYBIT_ERR_INVALID_ARG;
+    if (width < 0 || sequences < 0 || max_queries < 0 || max_length < 0 || x.groups < 0 || max_queries > (1 << 20)) return DYBIT_ERR_INVALID_ARG;
     if (x.groups && (x.table_width < 0 || x.max_queries < 0 || x.max_length < 0)) return DYBIT_ERR_INVALID_ARG;
     if (width > 0x7fffffff || x.table_width > 0x7fffffff) return DYBIT_ERR_INVALID_ARG;
     if (sequences > 0xffff || sequences * c.heads > 1 << 24 || x.groups > sequences) return DYBIT_ERR_INVALID_ARG;
@@ -80,7 +80,8 @@ dybit_status check_sizes(const dybit_heads &q, const dybit_kv_cache &c, int64_t 
 
 // ---- the join ---------------------------------------------------------------------------------------------------------------------
 // Row by row: the parts' maxima and sums, then their outputs, weighted.  One wave a row, or WAVES of them where a row has many
-// parts.  Bound by reading the parts, which are still in the last-level cache.
+// parts, each with every WAVES-th of them.  Bound by the latency of reading the parts, which are still in the caches: a wave asks for
+// eight of them at once.
 struct Join {
     Phase own, prefix;
     int32_t prefix_groups, own_slots, prefix_slots;
@@ -94,15 +95,15 @@ __device__ __forceinline__ void store_one(const Phase &p, int64_t at, float x)
 }
 
 template <int D, int WAVES>
-__global__ __launch_bounds__(kThreads) void join_kernel(const Join p)
+__global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : kThreads) void join_kernel(const Join p)
 {
-    constexpr int N = D / 64, ROWS = kWaves / WAVES;
+    constexpr int N = D / 64, ROWS = WAVES > 4 ? 1 : kWaves / WAVES, BATCH = 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = wave % WAVES;
     const int heads_q = p.own.kv_heads * p.own.group;
-    const int64_t n = (int64_t)blockIdx.x * ROWS + wave / WAVES;
+    const int n = (int)blockIdx.x * ROWS + wave / WAVES;
     const int seq = blockIdx.y;
     const Segment g = segment(p.own, seq);
-    const int i = (int)(n / heads_q), h = (int)(n - (int64_t)i * heads_q);
+    const int i = n / heads_q, h = n - i * heads_q;
     const bool real = i < g.count;
     const int64_t row = real ? (g.first + i) * heads_q + h : 0;
     int own = real ? (visible(p.own, g, i) + p.own.chunk - 1) / p.own.chunk : 0, before = 0;
@@ -120,14 +121,15 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Join p)
     }
     // the row's slots one after the other: those of the prefix, then its own
     const int count = before + own;
-    auto slot_of = [&](int j) { return (int64_t)(j < before ? j : p.prefix_slots + j - before); };
+    const int64_t base_slot = row * p.own.slots;
+    auto slot_of = [&](int j) { return base_slot + (j < before ? j : p.prefix_slots + j - before); };
     float m = -__builtin_inff(), l = 0.0f, x[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = 0.0f;
-    for (int j0 = part * 64; j0 < count; j0 += WAVES * 64) {
-        const int j = j0 + lane;
+    for (int j0 = 0; j0 < count; j0 += WAVES * 64) {
+        const int j = j0 + part + lane * WAVES;             // lane s: this wave's part s of the turn
         float2 stat = float2{-__builtin_inff(), 0.0f};
-        if (j < count) stat = *reinterpret_cast<const float2 *>(p.own.part_stat + 2 * (slot_of(j) * p.own.rows + row));
+        if (j < count) stat = *reinterpret_cast<const float2 *>(p.own.part_stat + 2 * slot_of(j));
         float top = stat.x;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
@@ -140,17 +142,25 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Join p)
         l = l * keep + sum;
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] *= keep;
-        const int end = count - j0 < 64 ? count - j0 : 64;
-        for (int s = 0; s < end; ++s) {
-            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s));
-            float y[N];
-            heads::Pack<float, N>::load(p.own.part_out + (slot_of(j0 + s) * p.own.rows + row) * D + N * lane, y);
+        const int mine = (count - j0 - part + WAVES - 1) / WAVES, end = mine < 64 ? mine : 64;
+        for (int s = 0; s < end; s += BATCH) {
+            float y[BATCH][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) x[k] += w * y[k];
+            for (int b = 0; b < BATCH; ++b) {
+                const int at = s + b < end ? s + b : end - 1;
+                heads::Pack<float, N>::load(p.own.part_out + slot_of(j0 + part + at * WAVES) * D + N * lane, y[b]);
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                if (s + b >= end) break;
+                const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s + b));
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] += w * y[b][k];
+            }
         }
     }
     if constexpr (WAVES > 1) {
-        __shared__ float s_m[kWaves], s_l[kWaves], s_x[kWaves][D];
+        __shared__ float s_m[WAVES * ROWS], s_l[WAVES * ROWS], s_x[WAVES * ROWS][D];
         if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
         heads::Pack<float, N>::store(&s_x[wave][N * lane], x);
         __syncthreads();
@@ -174,12 +184,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Join p)
 
 void join(const Join &j, int D, int64_t max_queries, int64_t sequences, hipStream_t st)
 {
-    // four waves a row where it may have more parts than a wave's lanes ask for at once in a few turns
-    const bool many = j.own_slots + j.prefix_slots > 16;
-    const int64_t rows = max_queries * j.own.kv_heads * j.own.group, per_block = many ? 1 : kWaves;
-    const dim3 grid((unsigned)((rows + per_block - 1) / per_block), (unsigned)sequences), block(kThreads);
-#define DYBIT_JOIN(D) if (many) hipLaunchKernelGGL((join_kernel<D, 4>), grid, block, 0, st, j); \
-                      else hipLaunchKernelGGL((join_kernel<D, 1>), grid, block, 0, st, j)
+    // waves a row: such that each has its parts in about one batch
+    const int slots = j.own_slots + j.prefix_slots, waves = slots <= 8 ? 1 : slots <= 48 ? 4 : 16;
+    const int64_t rows = max_queries * j.own.kv_heads * j.own.group, per_block = waves == 1 ? kWaves : 1;
+    const dim3 grid((unsigned)((rows + per_block - 1) / per_block), (unsigned)sequences);
+#define DYBIT_JOIN(D) if (waves == 1) hipLaunchKernelGGL((join_kernel<D, 1>), grid, dim3(kThreads), 0, st, j); \
+                      else if (waves == 4) hipLaunchKernelGGL((join_kernel<D, 4>), grid, dim3(kThreads), 0, st, j); \
+                      else hipLaunchKernelGGL((join_kernel<D, 16>), grid, dim3(1024), 0, st, j)
     if (D == 64) { DYBIT_JOIN(64); }
     else if (D == 128) { DYBIT_JOIN(128); }
     else { DYBIT_JOIN(256); }
@@ -243,7 +254,7 @@ extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, 
     p.scale = scale * 1.44269504088896340736f;
     p.part_out = need ? (float *)workspace : nullptr;
     p.part_stat = need ? (float *)workspace + (size_t)s.slots * (size_t)rows * (size_t)q.head_dim : nullptr;
-    p.rows = rows;
+    p.slots = s.slots;
     p.err = async_error_word();
     if (!p.err) return DYBIT_ERR_HIP;
     kv::Join j{};

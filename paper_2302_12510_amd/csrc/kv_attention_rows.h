@@ -112,7 +112,7 @@ template <int D>
 __device__ __forceinline__ void write_row(const Phase &p, int64_t row, int slot, int g4, const State<D> &st)
 {
     if (p.part_out) {
-        const int64_t at = (p.slot0 + slot) * p.rows + row;
+        const int64_t at = row * p.slots + p.slot0 + slot;
         if (g4 == 0) *reinterpret_cast<float2 *>(p.part_stat + 2 * at) = float2{st.m, st.l};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
