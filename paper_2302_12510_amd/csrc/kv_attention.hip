@@ -11,6 +11,8 @@
 // never change lanes.  Codes go from memory to registers to operands; no LDS in the loop.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kv_attention_rows.h"
 
 #ifndef DYBIT_KV_K
@@ -27,32 +29,74 @@ namespace {
 constexpr int KB = DYBIT_KV_K, VB = DYBIT_KV_V;
 constexpr int kThreads = 256, kWaves = 4;
 
-// 32 tokens of one key head as a lane holds them: codes of one token's run of keys and of eight tokens' values, and the scales.
+// 32 tokens of one key head as a lane holds them: codes of one token's run of keys, and of eight tokens' values; their scales.
 template <int D>
-struct Raw {
-    static constexpr int KW = D * KB / 128, VBYTES = D * VB / 128, VW = Values<VB, D / 16>::WORDS;
-    u32 k[2][KW];
-    u32 v[8][VW];
-    f32x4 sk[2], sv[2];
+struct Keys {
+    u32 w[2][D * KB / 128];
+    f32x4 scale[2];
+};
+template <int D>
+struct Vals {
+    static constexpr int BYTES = D * VB / 128;
+    u32 w[8][Values<VB, D / 16>::WORDS];
+    f32x4 scale[2];
 };
 
 template <int D, int TERMS, int NT>
 __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4;
-    const int head = blockIdx.x % p.kv_heads, seg = blockIdx.x / p.kv_heads;
-    const int64_t row0 = (int64_t)blockIdx.y * (16 * NT);
-    const int slot = blockIdx.z;
+    const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
+    const int row0 = (int)blockIdx.y * (16 * NT), slot = blockIdx.z;
     const Segment g = segment(p, seg);
     if (g.odd && head == 0 && blockIdx.y == 0 && slot == 0 && threadIdx.x == 0) *p.err = DYBIT_ERR_INVALID_ARG;
-    if (row0 >= (int64_t)g.count * p.group) return;
+    if (row0 >= g.count * p.group) return;
     // the keys of this workgroup: its chunk, as far as its last row sees
-    const int64_t last_row = row0 + 16 * NT - 1;
-    int last = (int)(last_row / p.group);
+    int last = (int)((unsigned)(row0 + 16 * NT - 1) / (unsigned)p.group);
     last = last < g.count ? last : g.count - 1;
     const int lo = slot * p.chunk, most = visible(p, g, last);
     const int hi = most - lo < p.chunk ? most : lo + p.chunk;
     if (lo >= hi && p.part_out) return;
+
+    // the pages of this wave's blocks of 16 tokens, one a lane: block j is step wave + 4 (j / 2), half j % 2
+    const int steps = (hi - lo + 31) >> 5;
+    const int32_t *table = p.tables + (int64_t)seg * p.table_width;
+    int page = -1;
+    {
+        const int token = lo + 32 * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
+        if (token < hi) {
+            page = table[token >> p.page_shift];
+            if (page < 0 || page >= p.pages) { page = -1; *p.err = DYBIT_ERR_INVALID_ARG; }
+        }
+    }
+    auto place_of = [&](int step, int b) {
+        const int id = max(__builtin_amdgcn_readlane(page, ((step - wave) >> 1) + b), 0);
+        return (((int64_t)id * p.kv_heads + head) << p.page_shift) + ((lo + 32 * step + 16 * b) & ((1 << p.page_shift) - 1));
+    };
+    const unsigned klane = (unsigned)((lane & 15) * (D * KB / 8) + g4 * (D * KB / 32)), vlane = (unsigned)(4 * g4 * (D * VB / 8) + (lane & 15) * Vals<D>::BYTES);
+    auto fetch_keys = [&](Keys<D> &k, int step) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int64_t place = place_of(step, b);
+            load_words<D * KB / 32>(p.k_codes + place * (D * KB / 8) + klane, k.w[b]);
+            k.scale[b] = *reinterpret_cast<const f32x4 *>(p.k_scales + place + 4 * g4);
+        }
+    };
+    auto fetch_values = [&](Vals<D> &v, int step) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int64_t place = place_of(step, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_words<Vals<D>::BYTES>(p.v_codes + place * (D * VB / 8) + i * (D * VB / 8) + vlane, v.w[4 * b + i]);
+            v.scale[b] = *reinterpret_cast<const f32x4 *>(p.v_scales + place + 4 * g4);
+        }
+    };
+    Keys<D> keys;
+    Vals<D> vals;
+    if (wave < steps) {
+        fetch_keys(keys, wave);
+        fetch_values(vals, wave);
+    }
 
     Rows<D, TERMS> r[NT];
     State<D> st[NT];
@@ -70,42 +114,10 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
     for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
     least = __builtin_amdgcn_readfirstlane(least);
 
-    // the pages of this wave's blocks of 16 tokens, one a lane: block j is step wave + 4 (j / 2), half j % 2
-    const int steps = (hi - lo + 31) >> 5;
-    const int32_t *table = p.tables + (int64_t)seg * p.table_width;
-    int page = -1;
-    {
-        const int token = lo + 32 * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
-        if (token < hi) {
-            page = table[token >> p.page_shift];
-            if (page < 0 || page >= p.pages) { page = -1; *p.err = DYBIT_ERR_INVALID_ARG; }
-        }
-    }
-    float vref = kFirstRef;
-    auto fetch = [&](Raw<D> &raw, int step) {
-        const int k = (step - wave) >> 2;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int id = max(__builtin_amdgcn_readlane(page, 2 * k + b), 0);
-            const int inside = (lo + 32 * step + 16 * b) & ((1 << p.page_shift) - 1);
-            const int64_t place = (((int64_t)id * p.kv_heads + head) << p.page_shift) + inside;
-            load_words<D * KB / 32>(p.k_codes + place * (D * KB / 8) + (lane & 15) * (D * KB / 8) + g4 * (D * KB / 32), raw.k[b]);
-            raw.sk[b] = *reinterpret_cast<const f32x4 *>(p.k_scales + place + 4 * g4);
-            raw.sv[b] = *reinterpret_cast<const f32x4 *>(p.v_scales + place + 4 * g4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                load_words<Raw<D>::VBYTES>(p.v_codes + place * (D * VB / 8) + (4 * g4 + i) * (D * VB / 8) + (lane & 15) * Raw<D>::VBYTES, raw.v[4 * b + i]);
-        }
-    };
-    auto go = [&](const Raw<D> &raw, int step) {
-        const int k = (step - wave) >> 2, token = lo + 32 * step;
-        int valid[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int left = hi - token - 16 * b;
-            valid[b] = __builtin_amdgcn_readlane(page, 2 * k + b) < 0 ? 0 : left < 16 ? left : 16;
-        }
-        const bool whole = valid[0] == 16 && valid[1] == 16 && token + 32 <= least;
+    float vref = kFirstRef, vup = kLargeP / kFirstRef;
+    // One step: the codes of the wave's next one are requested as soon as this one's have become operands.
+    auto go = [&](int step, auto more) {
+        const int token = lo + 32 * step;
         f32x4 s[NT][2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -113,45 +125,58 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
             for (int t = 0; t < NT; ++t) s[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
-                const f16x8 a = key_operand<KB>(raw.k[b], j);
+                const f16x8 a = key_operand<KB>(keys.w[b], j);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int e = 0; e < TERMS; ++e) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, r[t].q[e][j], s[t][b], 0, 0, 0);
             }
         }
-        // scales of the values; what lies past the end counts nothing, whatever it holds
-        float sv[8], top = 0.0f;
+        float x[NT][8], sv[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            sv[i] = whole || 4 * g4 + (i & 3) < valid[i >> 2] ? raw.sv[i >> 2][i & 3] : 0.0f;
-            top = fmaxf(top, sv[i]);
+            sv[i] = vals.scale[i >> 2][i & 3];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[t][i] = s[t][i >> 2][i & 3] * (keys.scale[i >> 2][i & 3] * r[t].factor);
         }
+        int valid[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int left = hi - token - 16 * b;
+            valid[b] = __builtin_amdgcn_readlane(page, ((step - wave) >> 1) + b) < 0 ? 0 : left < 16 ? left : 16;
+        }
+        if (valid[0] != 16 || valid[1] != 16 || token + 32 > least) {
+            // what lies past the end of the keys, or of what a row sees, counts nothing, whatever is there
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = 4 * g4 + (i & 3);
+                sv[i] = at < valid[i >> 2] ? sv[i] : 0.0f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) x[t][i] = at < valid[i >> 2] && token + 16 * (i >> 2) + at < r[t].seen ? x[t][i] : -__builtin_inff();
+            }
+            asm volatile("" ::: );                       // stays a branch: the whole steps pay nothing
+        }
+        if constexpr (decltype(more)::value) fetch_keys(keys, step + kWaves);
+        float top = 0.0f, shrink = 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, sv[i]);
         top = max_over_groups(top);
-        float shrink = 1.0f;
         if (__builtin_amdgcn_readfirstlane(__float_as_uint(top)) > __float_as_uint(vref)) {
             u32 e = (__float_as_uint(top) >> 23) + 1u;
             e = e > 240u ? 240u : e;
             const float ref = __uint_as_float(__builtin_amdgcn_readfirstlane(e) << 23);
             shrink = vref / ref;
             vref = ref;
+            vup = kLargeP / ref;
         }
-        const float up = kLargeP / vref;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sv[i] *= up;
+        for (int i = 0; i < 8; ++i) sv[i] *= vup;
         f16x8 prob[NT][TERMS];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float x[8], mx = -__builtin_inff();
+            float mx = x[t][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = s[t][i >> 2][i & 3] * (raw.sk[i >> 2][i & 3] * r[t].factor);
-                if (!whole) {
-                    const int at = 4 * g4 + (i & 3);
-                    x[i] = at < valid[i >> 2] && token + 16 * (i >> 2) + at < r[t].seen ? x[i] : -__builtin_inff();
-                }
-                mx = fmaxf(mx, x[i]);
-            }
+            for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[t][i]);
             const float m = fmaxf(st[t].m, max_over_groups(mx));
             const float base = m == -__builtin_inff() ? 0.0f : m;
             const float keep = __builtin_amdgcn_exp2f(st[t].m - base);
@@ -163,20 +188,20 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(x[i] - base);
-                st[t].l += x[i];
-                x[i] *= sv[i];
+                x[t][i] = __builtin_amdgcn_exp2f(x[t][i] - base);
+                st[t].l += x[t][i];
+                x[t][i] *= sv[i];
             }
             u32 w[TERMS][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if constexpr (TERMS == 2) split_pair(x[2 * i], x[2 * i + 1], w[0][i], w[1][i]);
-                else w[0][i] = round_pair(x[2 * i], x[2 * i + 1]);
+                if constexpr (TERMS == 2) split_pair(x[t][2 * i], x[t][2 * i + 1], w[0][i], w[1][i]);
+                else w[0][i] = round_pair(x[t][2 * i], x[t][2 * i + 1]);
             }
 #pragma unroll
             for (int e = 0; e < TERMS; ++e) prob[t][e] = operand(w[e][0], w[e][1], w[e][2], w[e][3]);
         }
-        const Values<VB, D / 16> values(raw.v);
+        const Values<VB, D / 16> values(vals.w);
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
             const f16x8 a = values.dim(j);
@@ -185,20 +210,12 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 #pragma unroll
                 for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][e], st[t].o[j], 0, 0, 0);
         }
+        if constexpr (decltype(more)::value) fetch_values(vals, step + kWaves);
     };
-    {
-        Raw<D> a, b;
+    if (wave < steps) {
         int step = wave;
-        if (step < steps) fetch(a, step);
-        while (step < steps) {
-            if (step + kWaves < steps) fetch(b, step + kWaves);
-            go(a, step);
-            step += kWaves;
-            if (step >= steps) break;
-            if (step + kWaves < steps) fetch(a, step + kWaves);
-            go(b, step);
-            step += kWaves;
-        }
+        for (; step + kWaves < steps; step += kWaves) go(step, std::true_type{});
+        go(step, std::false_type{});
     }
 
     // join the four waves: 2 and 3 into 0 and 1, then 1 into 0

@@ -71,9 +71,12 @@ dybit_status check_sizes(const dybit_heads &q, const dybit_kv_cache &c, int64_t 
     st = heads::check(q);
     if (st != DYBIT_OK) return st;
     if (c.layers != 1 || q.head_dim != c.head_dim || q.heads < c.heads || q.heads % c.heads) return DYBIT_ERR_INVALID_ARG;
-    if (width < 0 || sequences < 0 || max_queries < 0 || max_length < 0 || x.groups < 0 || max_queries > (1 << 20)) return DYBIT_ERR_INVALID_ARG;
+    if (width < 0 || sequences < 0 || max_queries < 0 || max_length < 0 || x.groups < 0) return DYBIT_ERR_INVALID_ARG;
     if (x.groups && (x.table_width < 0 || x.max_queries < 0 || x.max_length < 0)) return DYBIT_ERR_INVALID_ARG;
     if (width > 0x7fffffff || x.table_width > 0x7fffffff) return DYBIT_ERR_INVALID_ARG;
+    const int64_t most_rows = (int64_t)1 << 30;           // of a segment: row numbers are 32-bit
+    if (max_queries > most_rows || (x.groups && x.max_queries > most_rows)) return DYBIT_ERR_INVALID_ARG;
+    if (max_queries * (q.heads / c.heads) > most_rows || (x.groups && x.max_queries * (q.heads / c.heads) > most_rows)) return DYBIT_ERR_INVALID_ARG;
     if (sequences > 0xffff || sequences * c.heads > 1 << 24 || x.groups > sequences) return DYBIT_ERR_INVALID_ARG;
     return DYBIT_OK;
 }

@@ -9,29 +9,6 @@ namespace kv {
 constexpr float kLargeP = 16384.0f;                     // 2^14: what the largest probability times scale is brought to
 constexpr float kFirstRef = 7.88860905e-31f;            // 2^-100: the reference of the values' scales before any is seen
 
-__device__ __forceinline__ void load_query(const Phase &p, int64_t at, float (&x)[8])
-{
-    if (p.type == DYBIT_F32) {
-        const float *q = (const float *)p.q + at;
-        if (p.q_vectors) heads::Pack<float, 8>::load(q, x);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = q[i];
-    } else if (p.type == DYBIT_F16) {
-        const _Float16 *q = (const _Float16 *)p.q + at;
-        if (p.q_vectors) heads::Pack<_Float16, 8>::load(q, x);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (float)q[i];
-    } else {
-        const __bf16 *q = (const __bf16 *)p.q + at;
-        if (p.q_vectors) heads::Pack<__bf16, 8>::load(q, x);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (float)q[i];
-    }
-}
-
 template <int N>
 __device__ __forceinline__ void store_result(const Phase &p, int64_t at, const float (&x)[N])
 {
@@ -65,39 +42,73 @@ struct Rows {
     int64_t row;                                         // token * query heads + head; -1: no row
 };
 
+// TERMS is 2 for fp32 and 1 for the 16-bit types, whose words are converted after all of them have been requested.
 template <int KB, int D, int TERMS>
-__device__ __forceinline__ void load_rows(const Phase &p, const Segment &g, int head, int64_t first_row, int lane, Rows<D, TERMS> &r)
+__device__ __forceinline__ void load_rows(const Phase &p, const Segment &g, int head, int first_row, int lane, Rows<D, TERMS> &r)
 {
-    const int64_t n = first_row + (lane & 15);
-    const int i = (int)(n / p.group), h = head * p.group + (int)(n - (int64_t)i * p.group);
+    const unsigned n = (unsigned)(first_row + (lane & 15)), group = (unsigned)p.group;
+    const int i = (int)(n / group), h = head * p.group + (int)(n - (unsigned)i * group);
     const bool real = i < g.count;
     const int64_t token = g.first + i;
     r.row = real ? token * (p.kv_heads * p.group) + h : -1;
     r.seen = real ? visible(p, g, i) : 0;
     float x[D / 32][8];
-    float mx = 0.0f;
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
+    for (int j = 0; j < D / 32; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[j][e] = 0.0f;
-        if (real) load_query(p, token * p.q_token + h * p.q_head + (D / 4) * (lane >> 4) + 8 * j, x[j]);
+    if (real) {
+        const int64_t at = token * p.q_token + h * p.q_head + (D / 4) * (lane >> 4);
+        if constexpr (TERMS == 2) {
+            const float *q = (const float *)p.q + at;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                if (p.q_vectors) heads::Pack<float, 8>::load(q + 8 * j, x[j]);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[j][e] = q[8 * j + e];
+            }
+        } else {
+            typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+            const unsigned short *q = (const unsigned short *)p.q + at;
+            u16x8 w[D / 32];
+            if (p.q_vectors) {
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) w[j] = *reinterpret_cast<const u16x8 *>(q + 8 * j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[j][e] = q[8 * j + e];
+            }
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[j][e] = p.type == DYBIT_F16 ? (float)__builtin_bit_cast(_Float16, (unsigned short)w[j][e]) : __uint_as_float((u32)w[j][e] << 16);
+        }
+    }
+    float mx = 0.0f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[j][e]));
-    }
     mx = max_over_groups(mx);
     u32 e = __float_as_uint(mx) >> 23;
     e = e == 255u ? 127u + 14u : e < 15u ? 15u : e;      // infinities stay infinite
     const float up = __uint_as_float((254u + 14u - e) << 23);
     r.factor = p.scale * __uint_as_float((e - 14u) << 23) * fold<KB>();
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
+    for (int j = 0; j < D / 32; ++j) {
+        u32 w[TERMS][4];
 #pragma unroll
-        for (int i8 = 0; i8 < 8; ++i8) {
-            const float y = x[j][i8] * up;
-            const _Float16 hi = (_Float16)y;
-            r.q[0][j][i8] = hi;
-            if constexpr (TERMS == 2) r.q[1][j][i8] = (_Float16)(y - (float)hi);
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (TERMS == 2) split_pair(x[j][2 * k] * up, x[j][2 * k + 1] * up, w[0][k], w[1][k]);
+            else w[0][k] = round_pair(x[j][2 * k] * up, x[j][2 * k + 1] * up);
         }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) r.q[t][j] = operand(w[t][0], w[t][1], w[t][2], w[t][3]);
+    }
 }
 
 // Running state of 16 rows.

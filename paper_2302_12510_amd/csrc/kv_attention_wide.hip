@@ -47,13 +47,13 @@ __global__ __launch_bounds__(kThreads, D * TERMS > 128 ? 1 : 2) void attention_w
     constexpr int BUFFERS = D == 256 ? 1 : 2;            // 64 KB a step of 256 dims
     __shared__ Lds<D, BUFFERS> lds;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4;
-    const int head = blockIdx.x % p.kv_heads, seg = blockIdx.x / p.kv_heads;
-    const int64_t row0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * (16 * NT * kWaves);       // causal: those with the most keys first
+    const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
+    const int row0 = (int)(gridDim.y - 1 - blockIdx.y) * (16 * NT * kWaves);       // causal: those with the most keys first
     const int slot = blockIdx.z;
     const Segment g = segment(p, seg);
     if (g.odd && head == 0 && row0 == 0 && slot == 0 && threadIdx.x == 0) *p.err = DYBIT_ERR_INVALID_ARG;
-    if (row0 >= (int64_t)g.count * p.group) return;
-    int last = (int)((row0 + 16 * NT * kWaves - 1) / p.group);
+    if (row0 >= g.count * p.group) return;
+    int last = (int)((unsigned)(row0 + 16 * NT * kWaves - 1) / (unsigned)p.group);
     last = last < g.count ? last : g.count - 1;
     const int lo = slot * p.chunk, most = visible(p, g, last);
     const int hi = most - lo < p.chunk ? most : lo + p.chunk;

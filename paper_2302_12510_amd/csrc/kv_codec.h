@@ -20,12 +20,15 @@ typedef u32 u32x4 __attribute__((ext_vector_type(4)));
 
 template <int BITS> constexpr float fold() { return BITS == 8 ? 16384.0f : 1.0f; }
 
-// x: two 8-bit codes, each in both bytes of its half: the sign is the half's own sign bit then.
+// x: two 8-bit codes, each in both bytes of its half: the sign is the half's own sign bit then.  c, the low seven bits, is the
+// subnormal half c 2^-24, so one fma makes n = 2^7 - c on a scale of 2^-9 of it, whose bit pattern counts down as the code's value
+// counts up (dybit_codec.h): 13 exponents less the pattern is the value, 2^-14-fold.  Five instructions a pair with the
+// byte permute before it.
 __device__ __forceinline__ u32 halves_of_doubled(u32 x)
 {
-    const u32 h = (x & 0x007f007fu) | 0x64006400u;                                       // 1024 + c
-    const f16x2 n = (f16x2){(_Float16)1152.0f, (_Float16)1152.0f} - __builtin_bit_cast(f16x2, h);    // 2^7 - c
-    const u32 v = __builtin_bit_cast(u32, __builtin_bit_cast(u16x2, 0x58005800u) - __builtin_bit_cast(u16x2, n));
+    const f16x2 c = __builtin_bit_cast(f16x2, x & 0x007f007fu);
+    const f16x2 n = __builtin_elementwise_fma(c, (f16x2){(_Float16)-32768.0f, (_Float16)-32768.0f}, (f16x2){(_Float16)0.25f, (_Float16)0.25f});
+    const u32 v = __builtin_bit_cast(u32, __builtin_bit_cast(u16x2, 0x34003400u) - __builtin_bit_cast(u16x2, n));
     return v | (x & 0x80008000u);
 }
 
