@@ -14,11 +14,12 @@ constexpr int kThreads = 256, kWaves = 4;
 
 // ---- the plan ---------------------------------------------------------------------------------------------------------------------
 // Up to 32 rows of a segment are one or two tiles of a wave, whose waves share the keys of a chunk out; more go to the wide kernel,
-// whose waves share the rows out.  The tokens of a segment go to workgroups in chunks, as long ones as leave kEnough workgroups, were
-// all segments as long as the longest: short ones balance ragged batches and fill the device, long ones leave fewer partial
-// results (4 (D + 2) bytes a row and chunk, written and read back).
-constexpr int64_t kEnough = 1024, kEnoughWide = 512;
-constexpr int32_t kShortest = 128, kLongest = 4096;       // a wave holds the pages of 64 blocks of 16 tokens, a quarter of a chunk
+// whose waves share the rows out.  The tokens of a segment go to workgroups in chunks: as many as the device holds workgroups at once
+// (kHeld, by the kernels' registers), were all segments as long as the longest, since fewer leave it idle and more add their start and their
+// partial results (4 (D + 2) bytes a row, written and read back); but no longer ones than kLongest for few rows, which keeps batches of
+// very different lengths even.
+constexpr int64_t kHeld = 768, kHeldWide = 512;
+constexpr int32_t kShortest = 128, kLongest = 2048;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
 Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int64_t cap)
 {
@@ -27,10 +28,13 @@ Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int64_t ca
     p.tiles16 = max_rows > 16 && D < 256 ? 2 : 1;         // two tiles of 256 dims do not fit the registers
     const int64_t rows = p.wide ? kWideRows : 16 * p.tiles16;
     p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
-    const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles), enough = p.wide ? kEnoughWide : kEnough;
-    p.chunk = p.wide ? 1 << 30 : kLongest;
-    while (p.chunk > kShortest && base * std::max<int64_t>(1, (cap + p.chunk - 1) / p.chunk) < enough) p.chunk /= 2;
-    p.slots = std::max<int64_t>(1, (cap + p.chunk - 1) / p.chunk);
+    const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
+    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide : kHeld) / base);
+    int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
+    chunk = std::max<int64_t>(chunk, kShortest);
+    if (!p.wide) chunk = std::min<int64_t>(chunk, kLongest);
+    p.chunk = (int32_t)chunk;
+    p.slots = std::max<int64_t>(1, (cap + chunk - 1) / chunk);
     return p;
 }
 
