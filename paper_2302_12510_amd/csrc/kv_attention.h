@@ -83,7 +83,9 @@ void launch_wide_k8v8(const Phase &p, const Plan &plan, int D, int terms, int64_
 void launch_wide_k8v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
 void launch_wide_k4v8(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
 void launch_wide_k4v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
-constexpr int kWideRows = 128;                         // rows of a workgroup of the wide kernel
+// The wide kernel: rows of a wave, and waves of a workgroup.  Eight waves leave a wave 256 registers; four, 512.
+constexpr int kWideRows = 32;
+constexpr int wide_waves(int D, int terms) { return D * terms >= 256 ? 4 : 8; }
 
 }  // namespace kv
 }  // namespace dybit

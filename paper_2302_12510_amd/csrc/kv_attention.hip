@@ -104,17 +104,14 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         load_rows<KB, D, TERMS>(p, g, head, row0 + 16 * t, lane, r[t]);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) st[t].o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        st[t].m = -__builtin_inff();
-        st[t].l = 0.0f;
+        st[t].clear();
         if (r[t].row >= 0) least = min(least, r[t].seen);
     }
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
     least = __builtin_amdgcn_readfirstlane(least);
 
-    float vref = kFirstRef, vup = kLargeP / kFirstRef;
+    Reference ref;
     // One step: the codes of the wave's next one are requested as soon as this one's have become operands.
     auto go = [&](int step, auto more) {
         const int token = lo + 32 * step;
@@ -137,7 +134,7 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
         for (int i = 0; i < 8; ++i) {
             sv[i] = vals.scale[i >> 2][i & 3];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[t][i] = s[t][i >> 2][i & 3] * (keys.scale[i >> 2][i & 3] * r[t].factor);
+            for (int t = 0; t < NT; ++t) x[t][i] = s[t][i >> 2][i & 3] * keys.scale[i >> 2][i & 3];
         }
         int valid[2];
 #pragma unroll
@@ -157,50 +154,13 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
             asm volatile("" ::: );                       // stays a branch: the whole steps pay nothing
         }
         if constexpr (decltype(more)::value) fetch_keys(keys, step + kWaves);
-        float top = 0.0f, shrink = 1.0f;
+        float top = sv[0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, sv[i]);
-        top = max_over_groups(top);
-        if (__builtin_amdgcn_readfirstlane(__float_as_uint(top)) > __float_as_uint(vref)) {
-            u32 e = (__float_as_uint(top) >> 23) + 1u;
-            e = e > 240u ? 240u : e;
-            const float ref = __uint_as_float(__builtin_amdgcn_readfirstlane(e) << 23);
-            shrink = vref / ref;
-            vref = ref;
-            vup = kLargeP / ref;
-        }
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, sv[i]);
+        const float shrink = ref.raise(max_over_groups(top));
+        f16x8 prob[NT][1][TERMS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sv[i] *= vup;
-        f16x8 prob[NT][TERMS];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float mx = x[t][0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[t][i]);
-            const float m = fmaxf(st[t].m, max_over_groups(mx));
-            const float base = m == -__builtin_inff() ? 0.0f : m;
-            const float keep = __builtin_amdgcn_exp2f(st[t].m - base);
-            st[t].m = m;
-            if (__any(keep * shrink != 1.0f)) {
-                st[t].l *= keep;
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) st[t].o[j] *= keep * shrink;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[t][i] = __builtin_amdgcn_exp2f(x[t][i] - base);
-                st[t].l += x[t][i];
-                x[t][i] *= sv[i];
-            }
-            u32 w[TERMS][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (TERMS == 2) split_pair(x[t][2 * i], x[t][2 * i + 1], w[0][i], w[1][i]);
-                else w[0][i] = round_pair(x[t][2 * i], x[t][2 * i + 1]);
-            }
-#pragma unroll
-            for (int e = 0; e < TERMS; ++e) prob[t][e] = operand(w[e][0], w[e][1], w[e][2], w[e][3]);
-        }
+        for (int t = 0; t < NT; ++t) probabilities<D, TERMS, 8>(st[t], x[t], sv, r[t].factor, ref, shrink, prob[t]);
         const Values<VB, D / 16> values(vals.w);
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
@@ -208,7 +168,7 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][e], st[t].o[j], 0, 0, 0);
+                for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][0][e], st[t].o[j], 0, 0, 0);
         }
         if constexpr (decltype(more)::value) fetch_values(vals, step + kWaves);
     };
@@ -220,14 +180,8 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 
     // join the four waves: 2 and 3 into 0 and 1, then 1 into 0
     __shared__ float s_m[2][NT][16], s_l[2][NT][16], s_o[2][NT][D / 4][64];
-    const float back = vref / kLargeP * fold<VB>();
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        st[t].l += __shfl_xor(st[t].l, 16);
-        st[t].l += __shfl_xor(st[t].l, 32);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) st[t].o[j] *= back;
-    }
+    for (int t = 0; t < NT; ++t) settle<VB>(st[t], r[t].factor, ref);
 #pragma unroll
     for (int half = 2; half >= 1; half >>= 1) {
         if (wave >= half && wave < 2 * half) {

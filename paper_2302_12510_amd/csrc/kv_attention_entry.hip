@@ -18,18 +18,22 @@ constexpr int kThreads = 256, kWaves = 4;
 // (kHeld, by the kernels' registers), were all segments as long as the longest, since fewer leave it idle and more add their start and their
 // partial results (4 (D + 2) bytes a row, written and read back); but no longer ones than kLongest for few rows, which keeps batches of
 // very different lengths even.
-constexpr int64_t kHeld = 768, kHeldWide = 512;
+constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
 constexpr int32_t kShortest = 128, kLongest = 2048;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
-Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int64_t cap)
+// fp32 is split into two halves.
+int terms_of(int type) { return type == DYBIT_F32 ? 2 : 1; }
+
+Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, int64_t cap)
 {
     Plan p{};
     p.wide = max_rows > 32;
     p.tiles16 = max_rows > 16 && D < 256 ? 2 : 1;         // two tiles of 256 dims do not fit the registers
-    const int64_t rows = p.wide ? kWideRows : 16 * p.tiles16;
+    const int waves = wide_waves(D, terms_of(type));
+    const int64_t rows = p.wide ? kWideRows * waves : 16 * p.tiles16;
     p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
     const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
-    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide : kHeld) / base);
+    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide / waves : kHeld) / base);
     int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
     chunk = std::max<int64_t>(chunk, kShortest);
     if (!p.wide) chunk = std::min<int64_t>(chunk, kLongest);
@@ -56,10 +60,10 @@ Split split_of(const dybit_heads &q, const dybit_kv_cache &c, int64_t width, int
     Split s{};
     const int group = q.heads / c.heads;
     s.own_cap = cap_of(c, width, max_length);
-    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, s.own_cap);
+    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, q.type, s.own_cap);
     if (prefix.groups) {
         s.prefix_cap = cap_of(c, prefix.table_width, prefix.max_length);
-        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, s.prefix_cap);
+        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, q.type, s.prefix_cap);
         s.slots = s.own.slots + s.prefix.slots;
     } else {
         s.slots = s.own.slots > 1 ? s.own.slots : 0;
@@ -206,7 +210,7 @@ void join(const Join &j, int D, int64_t max_queries, int64_t sequences, hipStrea
 
 void launch(const Phase &p, const Plan &plan, const dybit_kv_cache &c, int64_t segments, hipStream_t st)
 {
-    const int terms = p.type == DYBIT_F32 ? 2 : 1;
+    const int terms = terms_of(p.type);
     const int widths = c.k_fmt.bits * 16 + c.v_fmt.bits;
     const auto run = plan.wide ? (widths == 8 * 16 + 8 ? launch_wide_k8v8 : widths == 8 * 16 + 4 ? launch_wide_k8v4 : widths == 4 * 16 + 8 ? launch_wide_k4v8 : launch_wide_k4v4)
                                : (widths == 8 * 16 + 8 ? launch_k8v8 : widths == 8 * 16 + 4 ? launch_k8v4 : widths == 4 * 16 + 8 ? launch_k4v8 : launch_k4v4);

@@ -7,7 +7,24 @@ namespace dybit {
 namespace kv {
 
 constexpr float kLargeP = 16384.0f;                     // 2^14: what the largest probability times scale is brought to
-constexpr float kFirstRef = 7.88860905e-31f;            // 2^-100: the reference of the values' scales before any is seen
+// The reference of the values' scales, a power of two: over the largest one seen, and 2^-90 at least, so that sums of
+// probabilities over it, times kLargeP, stay floats.
+constexpr int kFirstRefExponent = -90;
+
+// A larger reference for a largest scale of `top` (the same in all lanes): what the sums so far are to be multiplied by, else 1.
+struct Reference {
+    int exponent = kFirstRefExponent;
+    __device__ __forceinline__ float raise(float top)
+    {
+        const int e = (int)(__builtin_amdgcn_readfirstlane(__float_as_uint(fmaxf(top, 0.0f))) >> 23) - 126;      // 2^e > top
+        if (e <= exponent) return 1.0f;
+        const int to = e > 100 ? 100 : e, by = exponent - to;
+        exponent = to;
+        return by < -126 ? 0.0f : __uint_as_float((u32)(127 + by) << 23);
+    }
+    __device__ __forceinline__ float shift() const { return (float)(14 - exponent); }               // log2 of kLargeP over it
+    __device__ __forceinline__ float value() const { return __uint_as_float((u32)(127 + exponent - 14) << 23); }
+};
 
 template <int N>
 __device__ __forceinline__ void store_result(const Phase &p, int64_t at, const float (&x)[N])
@@ -37,7 +54,7 @@ __device__ __forceinline__ void store_result(const Phase &p, int64_t at, const f
 template <int D, int TERMS>
 struct Rows {
     f16x8 q[TERMS][D / 32];
-    float factor;
+    float factor;                                        // positive: log2(e) times the scale, whose sign the queries have taken
     int seen;                                            // keys that this lane's row sees
     int64_t row;                                         // token * query heads + head; -1: no row
 };
@@ -96,8 +113,8 @@ __device__ __forceinline__ void load_rows(const Phase &p, const Segment &g, int 
     mx = max_over_groups(mx);
     u32 e = __float_as_uint(mx) >> 23;
     e = e == 255u ? 127u + 14u : e < 15u ? 15u : e;      // infinities stay infinite
-    const float up = __uint_as_float((254u + 14u - e) << 23);
-    r.factor = p.scale * __uint_as_float((e - 14u) << 23) * fold<KB>();
+    const float up = __uint_as_float(((254u + 14u - e) << 23) | (__float_as_uint(p.scale) & 0x80000000u));
+    r.factor = fmaxf(fabsf(p.scale) * __uint_as_float((e - 14u) << 23) * fold<KB>(), 1.17549435e-38f);
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
         u32 w[TERMS][4];
@@ -111,12 +128,70 @@ __device__ __forceinline__ void load_rows(const Phase &p, const Segment &g, int 
     }
 }
 
-// Running state of 16 rows.
+// Running state of 16 rows: results and sums of the probabilities are over the reference of the values' scales, times kLargeP; the
+// maximum is that of the scores before their factor.
 template <int D>
 struct State {
     f32x4 o[D / 16];
     float m, l;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        m = -__builtin_inff();
+        l = 0.0f;
+    }
 };
+
+// N scores of a lane's row (before their factor; -inf: not seen) to probabilities times their values' scales, as operands of eight.
+template <int D, int TERMS, int N>
+__device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const float (&sv)[N], float factor, const Reference &ref, float shrink,
+                                              f16x8 (&prob)[N / 8][TERMS])
+{
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[i]);
+    const float m = fmaxf(st.m, max_over_groups(mx));
+    const float base = m == -__builtin_inff() ? 0.0f : m;
+    const float keep = __builtin_amdgcn_exp2f((st.m - base) * factor) * shrink;
+    st.m = m;
+    if (__any(keep != 1.0f)) {
+        st.l *= keep;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st.o[j] *= keep;
+    }
+    const float add = ref.shift() - base * factor;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], factor, add));
+        st.l += x[i];
+        x[i] *= sv[i];
+    }
+#pragma unroll
+    for (int c = 0; c < N / 8; ++c) {
+        u32 w[TERMS][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TERMS == 2) split_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], w[0][i], w[1][i]);
+            else w[0][i] = round_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
+        }
+#pragma unroll
+        for (int e = 0; e < TERMS; ++e) prob[c][e] = operand(w[e][0], w[e][1], w[e][2], w[e][3]);
+    }
+}
+
+// The state in units of its own: over all lanes of a row, without the reference and the fold of the codes.
+template <int VB, int D>
+__device__ __forceinline__ void settle(State<D> &st, float factor, const Reference &ref)
+{
+    st.l += __shfl_xor(st.l, 16);
+    st.l += __shfl_xor(st.l, 32);
+    st.l *= ref.value();
+    st.m *= factor;
+    const float back = ref.value() * fold<VB>();
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) st.o[j] *= back;
+}
 
 // A row's result, or its part of one: a lane has dims (D / 16) (4 g4 + i) + j of its row.
 template <int D>

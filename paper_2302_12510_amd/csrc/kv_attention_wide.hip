@@ -1,10 +1,11 @@
 // Attention over the cache of codes for many rows of queries (chunks of prompts, the queries of a group over its prefix); one build
 // per pair of code widths (DYBIT_KV_K, DYBIT_KV_V).
 //
-// The arithmetic is kv_attention.hip's.  Here four waves hold 32 rows each and go through the same keys together: a step is 64 tokens,
-// of which every wave decodes a quarter and leaves it in LDS as operands of the matrix instruction, 16 bytes a lane in lane order
-// (no bank conflicts, no padding); all four read them all.  Decoding, some 2.5 instructions a code, is shared by 128 rows then.
-// The next step's codes are requested before this step's products and decoded behind them, into the other half of the LDS.
+// The arithmetic is kv_attention.hip's.  Here the waves of a workgroup hold 32 rows each and go through the same keys together: of a step,
+// 16 tokens a wave, every wave decodes its share and leaves it in LDS as operands of the matrix instruction, 16 bytes a lane in lane
+// order (no bank conflicts, no padding); all of them read them all.  So decoding, some 2.5 instructions a code, is shared by the
+// rows of eight waves (four where a wave needs more than 256 registers).  The next step's codes are requested before this step's
+// products and decoded behind them, into the other half of the LDS.
 #include <hip/hip_runtime.h>
 
 #include "kv_attention_rows.h"
@@ -21,95 +22,80 @@ namespace kv {
 namespace {
 
 constexpr int KB = DYBIT_KV_K, VB = DYBIT_KV_V;
-constexpr int kThreads = 256, kWaves = 4, kStep = 64, kBlocks = kStep / 16, NT = kWideRows / (16 * kWaves);
+constexpr int NT = kWideRows / 16, kSub = 64, kSubBlocks = kSub / 16;     // tiles of a wave; tokens whose scores a wave holds at a time
 
 // What a wave decodes of a step: the keys of 16 tokens, half the dims of the values of 32, and the scales of 16.
 template <int D>
 struct Share {
-    static constexpr int KW = D * KB / 128, VBYTES = D * VB / 256, VW = Values<VB, D / 32>::WORDS;
-    u32 k[KW];
-    u32 v[8][VW];
+    static constexpr int VBYTES = D * VB / 256;
+    u32 k[D * KB / 128];
+    u32 v[8][Values<VB, D / 32>::WORDS];
     float scale;                                         // lanes 0 to 15: of the keys, 16 to 31: of the values
     int valid;                                           // tokens of the block of 16 that count
 };
 
-template <int D, int BUFFERS>
+template <int D, int WAVES, int BUFFERS>
 struct Lds {
-    f16x8 k[BUFFERS][kBlocks][D / 32][64];
-    f16x8 v[BUFFERS][2][D / 16][64];
-    float sk[BUFFERS][kStep], sv[BUFFERS][kStep];
-    int valid[BUFFERS][kBlocks];
+    f16x8 k[BUFFERS][WAVES][D / 32][64];
+    f16x8 v[BUFFERS][WAVES / 2][D / 16][64];
+    float sk[BUFFERS][16 * WAVES], sv[BUFFERS][16 * WAVES];
+    float top[BUFFERS][WAVES];                           // largest scale of a block's values
+    int valid[BUFFERS][WAVES];
 };
 
 template <int D, int TERMS>
-__global__ __launch_bounds__(kThreads, D * TERMS > 128 ? 1 : 2) void attention_wide_kernel(const Phase p)
+__global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4) void attention_wide_kernel(const Phase p)
 {
+    constexpr int WAVES = wide_waves(D, TERMS), STEP = 16 * WAVES;
     constexpr int BUFFERS = D == 256 ? 1 : 2;            // 64 KB a step of 256 dims
-    __shared__ Lds<D, BUFFERS> lds;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4;
+    __shared__ Lds<D, WAVES, BUFFERS> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
-    const int row0 = (int)(gridDim.y - 1 - blockIdx.y) * (16 * NT * kWaves);       // causal: those with the most keys first
+    const int row0 = (int)(gridDim.y - 1 - blockIdx.y) * (16 * NT * WAVES);        // causal: those with the most keys first
     const int slot = blockIdx.z;
     const Segment g = segment(p, seg);
     if (g.odd && head == 0 && row0 == 0 && slot == 0 && threadIdx.x == 0) *p.err = DYBIT_ERR_INVALID_ARG;
     if (row0 >= g.count * p.group) return;
-    int last = (int)((unsigned)(row0 + 16 * NT * kWaves - 1) / (unsigned)p.group);
+    int last = (int)((unsigned)(row0 + 16 * NT * WAVES - 1) / (unsigned)p.group);
     last = last < g.count ? last : g.count - 1;
     const int lo = slot * p.chunk, most = visible(p, g, last);
     const int hi = most - lo < p.chunk ? most : lo + p.chunk;
     if (lo >= hi && p.part_out) return;
 
-    Rows<D, TERMS> r[NT];
-    State<D> st[NT];
-    int least = 0x7fffffff;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        load_rows<KB, D, TERMS>(p, g, head, row0 + 16 * (NT * wave + t), lane, r[t]);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) st[t].o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        st[t].m = -__builtin_inff();
-        st[t].l = 0.0f;
-        if (r[t].row >= 0) least = min(least, r[t].seen);
-    }
-#pragma unroll
-    for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
-    least = __builtin_amdgcn_readfirstlane(least);
-
-    const int steps = (hi - lo + kStep - 1) / kStep;
+    const int steps = (hi - lo + STEP - 1) / STEP;
     const int32_t *table = p.tables + (int64_t)seg * p.table_width;
-    const int vchunk = wave >> 1, vhalf = wave & 1;
-    auto page_of = [&](int token) {                      // of a block of 16 tokens; -1: none that counts
-        int id = -1;
+    // pages of the next 32 steps' blocks that this wave decodes, a lane each: its own (even lanes), and the one beside it, with which it
+    // shares 32 tokens' values; -1: none that counts
+    const int beside = wave ^ 1;
+    int pages = -1;
+    auto look = [&](int step) {
+        const int token = lo + (step + (lane >> 1)) * STEP + 16 * (lane & 1 ? beside : wave);
+        pages = -1;
         if (token < hi) {
-            id = table[token >> p.page_shift];
-            if (id < 0 || id >= p.pages) { id = -1; *p.err = DYBIT_ERR_INVALID_ARG; }
+            pages = table[token >> p.page_shift];
+            if (pages < 0 || pages >= p.pages) { pages = -1; *p.err = DYBIT_ERR_INVALID_ARG; }
         }
-        return __builtin_amdgcn_readfirstlane(id);
     };
     auto place_of = [&](int id, int token) {
         return (((int64_t)max(id, 0) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
     };
-    int kid = -1, vid[2] = {-1, -1};                     // pages of the next step's blocks that this wave decodes
-    auto look = [&](int step) {
-        const int token = lo + step * kStep;
-        kid = page_of(token + 16 * wave);
-        vid[0] = page_of(token + 32 * vchunk);
-        vid[1] = page_of(token + 32 * vchunk + 16);
-    };
+    const unsigned klane = (unsigned)((lane & 15) * (D * KB / 8) + g4 * (D * KB / 32));
+    const unsigned vlane = (unsigned)(4 * g4 * (D * VB / 8) + (lane & 15) * (D * VB / 128) + (wave & 1) * Share<D>::VBYTES);
     auto fetch = [&](Share<D> &s, int step) {
-        const int token = lo + step * kStep;
-        const int64_t kp = place_of(kid, token + 16 * wave);
+        if ((step & 31) == 0) look(step);
+        const int token = lo + step * STEP, at = 2 * (step & 31);
+        const int own = __builtin_amdgcn_readlane(pages, at), other = __builtin_amdgcn_readlane(pages, at + 1);
+        const int64_t kp = place_of(own, token + 16 * wave), op = place_of(other, token + 16 * beside);
         const int left = hi - token - 16 * wave;
-        s.valid = kid < 0 ? 0 : left < 16 ? left : 16;
-        load_words<D * KB / 32>(p.k_codes + kp * (D * KB / 8) + (lane & 15) * (D * KB / 8) + g4 * (D * KB / 32), s.k);
+        s.valid = own < 0 ? 0 : left < 16 ? left : 16;
+        load_words<D * KB / 32>(p.k_codes + kp * (D * KB / 8) + klane, s.k);
         s.scale = 0.0f;
         if ((lane & 15) < s.valid && lane < 32) s.scale = (lane < 16 ? p.k_scales : p.v_scales)[kp + (lane & 15)];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const int64_t vp = place_of(vid[b], token + 32 * vchunk + 16 * b);
+            const uint8_t *v = p.v_codes + ((wave & 1) == b ? kp : op) * (D * VB / 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                load_words<Share<D>::VBYTES>(p.v_codes + (vp + 4 * g4 + i) * (D * VB / 8) + (lane & 15) * (D * VB / 128) + vhalf * Share<D>::VBYTES, s.v[4 * b + i]);
+            for (int i = 0; i < 4; ++i) load_words<Share<D>::VBYTES>(v + i * (D * VB / 8) + vlane, s.v[4 * b + i]);
         }
     };
     auto decode = [&](const Share<D> &s, int buffer) {
@@ -117,142 +103,119 @@ __global__ __launch_bounds__(kThreads, D * TERMS > 128 ? 1 : 2) void attention_w
         for (int j = 0; j < D / 32; ++j) lds.k[buffer][wave][j][lane] = key_operand<KB>(s.k, j);
         const Values<VB, D / 32> values(s.v);
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) lds.v[buffer][vchunk][vhalf * (D / 32) + j][lane] = values.dim(j);
+        for (int j = 0; j < D / 32; ++j) lds.v[buffer][wave >> 1][(wave & 1) * (D / 32) + j][lane] = values.dim(j);
         if (lane < 16) lds.sk[buffer][16 * wave + lane] = s.scale;
         else if (lane < 32) lds.sv[buffer][16 * wave + lane - 16] = s.scale;
-        if (lane == 0) lds.valid[buffer][wave] = s.valid;
+        const float top = max_over_row(s.scale);
+        if (lane == 16) {
+            lds.top[buffer][wave] = top;
+            lds.valid[buffer][wave] = s.valid;
+        }
     };
-    float vref = kFirstRef, vup = kLargeP / kFirstRef;
-    auto go = [&](int step, int buffer) {
-        const int token = lo + step * kStep;
-        f32x4 s[NT][kBlocks];
+    Share<D> share;
+    if (steps > 0) fetch(share, 0);
+
+    Rows<D, TERMS> r[NT];
+    State<D> st[NT];
+    int least = 0x7fffffff;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
+    for (int t = 0; t < NT; ++t) {
+        load_rows<KB, D, TERMS>(p, g, head, row0 + 16 * (NT * wave + t), lane, r[t]);
+        st[t].clear();
+        if (r[t].row >= 0) least = min(least, r[t].seen);
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
+    least = __builtin_amdgcn_readfirstlane(least);
+    const bool works = row0 + 16 * NT * wave < g.count * p.group;      // waves without rows only decode
+
+    Reference ref;
+    auto go = [&](int token, int buffer, int sub) {
+        f32x4 s[NT][kSubBlocks];
+#pragma unroll
+        for (int b = 0; b < kSubBlocks; ++b) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) s[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
-                const f16x8 a = lds.k[buffer][b][j][lane];
+                const f16x8 a = lds.k[buffer][sub * kSubBlocks + b][j][lane];
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int e = 0; e < TERMS; ++e) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, r[t].q[e][j], s[t][b], 0, 0, 0);
             }
         }
-        float sv[4 * kBlocks], sk[4 * kBlocks], top = 0.0f;
-        int valid[kBlocks];
-        bool whole = token + kStep <= least;
+        constexpr int N = 4 * kSubBlocks;
+        float x[NT][N], sv[N];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(&lds.sv[buffer][16 * b + 4 * g4]), y = *reinterpret_cast<const f32x4 *>(&lds.sk[buffer][16 * b + 4 * g4]);
+        for (int b = 0; b < kSubBlocks; ++b) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(&lds.sv[buffer][sub * kSub + 16 * b + 4 * g4]), k = *reinterpret_cast<const f32x4 *>(&lds.sk[buffer][sub * kSub + 16 * b + 4 * g4]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                sv[4 * b + i] = x[i];
-                sk[4 * b + i] = y[i];
-                top = fmaxf(top, x[i]);
+                sv[4 * b + i] = v[i];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) x[t][4 * b + i] = s[t][b][i] * k[i];
             }
-            valid[b] = lds.valid[buffer][b];
-            whole = whole && __builtin_amdgcn_readfirstlane(valid[b]) == 16;
         }
-        top = max_over_groups(top);
-        float shrink = 1.0f;
-        if (__builtin_amdgcn_readfirstlane(__float_as_uint(top)) > __float_as_uint(vref)) {
-            u32 e = (__float_as_uint(top) >> 23) + 1u;
-            e = e > 240u ? 240u : e;
-            const float ref = __uint_as_float(__builtin_amdgcn_readfirstlane(e) << 23);
-            shrink = vref / ref;
-            vref = ref;
-            vup = kLargeP / ref;
-        }
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 valid = *reinterpret_cast<const i32x4 *>(&lds.valid[buffer][sub * kSubBlocks]);
+        const f32x4 tops = *reinterpret_cast<const f32x4 *>(&lds.top[buffer][sub * kSubBlocks]);
+        if (__builtin_amdgcn_readfirstlane(min(min(valid[0], valid[1]), min(valid[2], valid[3]))) < 16 || token + kSub > least) {
+            // what lies past the end of the keys, or of what a row sees, counts nothing (the scales there are zero already)
 #pragma unroll
-        for (int i = 0; i < 4 * kBlocks; ++i) sv[i] *= vup;
-        f16x8 prob[NT][2][TERMS];
+            for (int i = 0; i < N; ++i) {
+                const int at = 4 * g4 + (i & 3);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float x[4 * kBlocks], mx = -__builtin_inff();
-#pragma unroll
-            for (int i = 0; i < 4 * kBlocks; ++i) {
-                x[i] = s[t][i >> 2][i & 3] * (sk[i] * r[t].factor);
-                if (!whole) {
-                    const int at = 4 * g4 + (i & 3);
-                    x[i] = at < valid[i >> 2] && token + 16 * (i >> 2) + at < r[t].seen ? x[i] : -__builtin_inff();
+                for (int t = 0; t < NT; ++t) {
+                    const int end = min(valid[i >> 2], r[t].seen - token - 16 * (i >> 2));
+                    x[t][i] = at < end ? x[t][i] : -__builtin_inff();
                 }
-                mx = fmaxf(mx, x[i]);
             }
-            const float m = fmaxf(st[t].m, max_over_groups(mx));
-            const float base = m == -__builtin_inff() ? 0.0f : m;
-            const float keep = __builtin_amdgcn_exp2f(st[t].m - base);
-            st[t].m = m;
-            if (__any(keep * shrink != 1.0f)) {
-                st[t].l *= keep;
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) st[t].o[j] *= keep * shrink;
-            }
-#pragma unroll
-            for (int i = 0; i < 4 * kBlocks; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(x[i] - base);
-                st[t].l += x[i];
-                x[i] *= sv[i];
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                u32 w[TERMS][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (TERMS == 2) split_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], w[0][i], w[1][i]);
-                    else w[0][i] = round_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
-                }
-#pragma unroll
-                for (int e = 0; e < TERMS; ++e) prob[t][c][e] = operand(w[e][0], w[e][1], w[e][2], w[e][3]);
-            }
+            asm volatile("" ::: );                       // stays a branch: the whole steps pay nothing
         }
+        const float shrink = ref.raise(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+        f16x8 prob[NT][N / 8][TERMS];
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int t = 0; t < NT; ++t) probabilities<D, TERMS, N>(st[t], x[t], sv, r[t].factor, ref, shrink, prob[t]);
+#pragma unroll
+        for (int c = 0; c < N / 8; ++c)
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
-                const f16x8 a = lds.v[buffer][c][j][lane];
+                const f16x8 a = lds.v[buffer][sub * (N / 8) + c][j][lane];
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][c][e], st[t].o[j], 0, 0, 0);
             }
     };
-    Share<D> share;
-    if (steps > 0) {
-        look(0);
-        fetch(share, 0);
-        look(1);
-        decode(share, 0);
-    }
+    if (steps > 0) decode(share, 0);
     __syncthreads();
     for (int step = 0; step < steps; ++step) {
         const bool more = step + 1 < steps;
-        if (more) {
-            fetch(share, step + 1);
-            look(step + 2);
+        const int buffer = step & (BUFFERS - 1), token = lo + step * STEP;
+        if (more) fetch(share, step + 1);
+        if (works) {
+#pragma unroll 1
+            for (int sub = 0; sub < STEP / kSub; ++sub)
+                if (token + sub * kSub < hi) go(token + sub * kSub, buffer, sub);
         }
-        go(step, step & (BUFFERS - 1));
         if (BUFFERS == 1) __syncthreads();
         if (more) decode(share, (step + 1) & (BUFFERS - 1));
         __syncthreads();
     }
 
-    const float back = vref / kLargeP * fold<VB>();
+    if (!works) return;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        if (r[t].row < 0) continue;                      // lanes of a row are all here or all not: their sums go over lanes 16 and 32 apart
-        st[t].l += __shfl_xor(st[t].l, 16);
-        st[t].l += __shfl_xor(st[t].l, 32);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) st[t].o[j] *= back;
-        write_row<D>(p, r[t].row, slot, g4, st[t]);
+        settle<VB>(st[t], r[t].factor, ref);
+        if (r[t].row >= 0) write_row<D>(p, r[t].row, slot, g4, st[t]);
     }
 }
 
 template <int D>
 void launch_d(const Phase &p, const Plan &plan, int terms, int64_t segments, hipStream_t st)
 {
-    const dim3 grid((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots), block(kThreads);
+    const dim3 grid((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots), block((unsigned)(64 * wide_waves(D, terms)));
     if (terms == 1) hipLaunchKernelGGL((attention_wide_kernel<D, 1>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((attention_wide_kernel<D, 2>), grid, block, 0, st, p);
 }

@@ -145,5 +145,14 @@ __device__ __forceinline__ float max_over_groups(float x)
     return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
+// The largest of a value over a lane's row of 16.
+__device__ __forceinline__ float max_over_row(float x)
+{
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, true)));   // row_ror:8
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, true)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, true)));
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, true)));
+}
+
 }  // namespace kv
 }  // namespace dybit
