@@ -6,10 +6,16 @@
 namespace dybit {
 namespace kv {
 
-constexpr float kLargeP = 16384.0f;                     // 2^14: what the largest probability times scale is brought to
-// The reference of the values' scales, a power of two: over the largest one seen, and 2^-90 at least, so that sums of
-// probabilities over it, times kLargeP, stay floats.
-constexpr int kFirstRefExponent = -90;
+// A probability times its value's scale becomes an operand over a power of two (Reference) and over the probability of a score that
+// is at most kSlack powers of two under the row's largest: the running maximum is only moved when a score passes it by more, which
+// saves most of the multiplications of the results so far.  Operands stay under 2^(kLarge + kSlack), which is under the largest
+// half, and as far up as that allows: the keys that count least keep most bits so.
+constexpr int kLarge = 14;
+constexpr float kSlack = 1.75f;
+
+// The reference of the values' scales, a power of two: over the largest one seen, and 2^-80 at least, so that sums of
+// probabilities over it, times 2^kLarge, stay floats.
+constexpr int kFirstRefExponent = -80;
 
 // A larger reference for a largest scale of `top` (the same in all lanes): what the sums so far are to be multiplied by, else 1.
 struct Reference {
@@ -22,8 +28,8 @@ struct Reference {
         exponent = to;
         return by < -126 ? 0.0f : __uint_as_float((u32)(127 + by) << 23);
     }
-    __device__ __forceinline__ float shift() const { return (float)(14 - exponent); }               // log2 of kLargeP over it
-    __device__ __forceinline__ float value() const { return __uint_as_float((u32)(127 + exponent - 14) << 23); }
+    __device__ __forceinline__ float shift() const { return (float)(kLarge - exponent); }           // log2 of 2^kLarge over it
+    __device__ __forceinline__ float value() const { return __uint_as_float((u32)(127 + exponent - kLarge) << 23); }
 };
 
 template <int N>
@@ -128,18 +134,18 @@ __device__ __forceinline__ void load_rows(const Phase &p, const Segment &g, int 
     }
 }
 
-// Running state of 16 rows: results and sums of the probabilities are over the reference of the values' scales, times kLargeP; the
-// maximum is that of the scores before their factor.
+// Running state of 16 rows: results and sums of the probabilities are over the reference of the values' scales, times 2^kLarge; m, the
+// maximum up to the slack, is of scores before their factor, and a score x counts 2^(x factor + add).
 template <int D>
 struct State {
     f32x4 o[D / 16];
-    float m, l;
+    float m, l, add;
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         m = -__builtin_inff();
-        l = 0.0f;
+        l = add = 0.0f;
     }
 };
 
@@ -151,19 +157,20 @@ __device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[i]);
-    const float m = fmaxf(st.m, max_over_groups(mx));
-    const float base = m == -__builtin_inff() ? 0.0f : m;
-    const float keep = __builtin_amdgcn_exp2f((st.m - base) * factor) * shrink;
-    st.m = m;
-    if (__any(keep != 1.0f)) {
+    mx = max_over_groups(mx);
+    const bool over = (mx - st.m) * factor > kSlack;       // before anything is seen: infinitely, or (nothing here either) not a number
+    if (__any(over) || shrink != 1.0f) {
+        const float m = over ? mx : st.m;
+        const float keep = (over ? __builtin_amdgcn_exp2f((st.m - m) * factor) : 1.0f) * shrink;
+        st.m = m;
+        st.add = m == -__builtin_inff() ? 0.0f : ref.shift() - m * factor;
         st.l *= keep;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) st.o[j] *= keep;
     }
-    const float add = ref.shift() - base * factor;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], factor, add));
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], factor, st.add));
         st.l += x[i];
         x[i] *= sv[i];
     }

@@ -188,19 +188,25 @@ __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4
                     for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][c][e], st[t].o[j], 0, 0, 0);
             }
     };
-    if (steps > 0) decode(share, 0);
+    // Half of the waves decode the next step before this one's products and half behind them: while some of a SIMD's waves use the
+    // vector unit, the others use the matrix unit.
+    const bool early = wave >= WAVES / 2;
+    auto prepare = [&](int step) {                       // codes of `step` are in registers
+        if (step < steps) decode(share, step & (BUFFERS - 1));
+        if (step + 1 < steps) fetch(share, step + 1);
+    };
+    prepare(0);
     __syncthreads();
     for (int step = 0; step < steps; ++step) {
-        const bool more = step + 1 < steps;
         const int buffer = step & (BUFFERS - 1), token = lo + step * STEP;
-        if (more) fetch(share, step + 1);
+        if (BUFFERS == 2 && early) prepare(step + 1);
         if (works) {
 #pragma unroll 1
             for (int sub = 0; sub < STEP / kSub; ++sub)
                 if (token + sub * kSub < hi) go(token + sub * kSub, buffer, sub);
         }
         if (BUFFERS == 1) __syncthreads();
-        if (more) decode(share, (step + 1) & (BUFFERS - 1));
+        if (BUFFERS == 1 || !early) prepare(step + 1);
         __syncthreads();
     }
 
