@@ -144,14 +144,19 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
         }
         if (valid[0] != 16 || valid[1] != 16 || token + 32 > least) {
             // what lies past the end of the keys, or of what a row sees, counts nothing, whatever is there
+            int at = 4 * g4;
+            asm volatile("" : "+v"(at));                   // keeps all of it behind its branch: whole steps pay nothing
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = 4 * g4 + (i & 3);
-                sv[i] = at < valid[i >> 2] ? sv[i] : 0.0f;
+            for (int b = 0; b < 2; ++b) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) x[t][i] = at < valid[i >> 2] && token + 16 * (i >> 2) + at < r[t].seen ? x[t][i] : -__builtin_inff();
+                for (int i = 0; i < 4; ++i) sv[4 * b + i] = at + i < valid[b] ? sv[4 * b + i] : 0.0f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int left = min(valid[b], r[t].seen - token - 16 * b) - at;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][4 * b + i] = i < left ? x[t][4 * b + i] : -__builtin_inff();
+                }
             }
-            asm volatile("" ::: );                       // stays a branch: the whole steps pay nothing
         }
         if constexpr (decltype(more)::value) fetch_keys(keys, step + kWaves);
         float top = sv[0];
@@ -160,7 +165,10 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
         const float shrink = ref.raise(max_over_groups(top));
         f16x8 prob[NT][1][TERMS];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) probabilities<D, TERMS, 8>(st[t], x[t], sv, r[t].factor, ref, shrink, prob[t]);
+        for (int t = 0; t < NT; ++t) {
+            raise_maximum<D, 8>(st[t], x[t], r[t].factor, ref, shrink);
+            probabilities<D, TERMS, 8>(st[t], x[t], sv, r[t].factor, prob[t]);
+        }
         const Values<VB, D / 16> values(vals.w);
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {

@@ -149,16 +149,16 @@ struct State {
     }
 };
 
-// N scores of a lane's row (before their factor; -inf: not seen) to probabilities times their values' scales, as operands of eight.
-template <int D, int TERMS, int N>
-__device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const float (&sv)[N], float factor, const Reference &ref, float shrink,
-                                              f16x8 (&prob)[N / 8][TERMS])
+// N scores of a lane's row (before their factor; -inf: not seen) against its running maximum.  Before anything is seen a score is
+// infinitely over it, or (nothing here either) not a number more.
+template <int D, int N>
+__device__ __forceinline__ void raise_maximum(State<D> &st, const float (&x)[N], float factor, const Reference &ref, float shrink)
 {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[i]);
     mx = max_over_groups(mx);
-    const bool over = (mx - st.m) * factor > kSlack;       // before anything is seen: infinitely, or (nothing here either) not a number
+    const bool over = (mx - st.m) * factor > kSlack;
     if (__any(over) || shrink != 1.0f) {
         const float m = over ? mx : st.m;
         const float keep = (over ? __builtin_amdgcn_exp2f((st.m - m) * factor) : 1.0f) * shrink;
@@ -168,6 +168,12 @@ __device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) st.o[j] *= keep;
     }
+}
+
+// Then: scores to probabilities times their values' scales, as operands of eight.
+template <int D, int TERMS, int N>
+__device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const float (&sv)[N], float factor, f16x8 (&prob)[N / 8][TERMS])
+{
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], factor, st.add));

@@ -162,21 +162,24 @@ __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4
         const f32x4 tops = *reinterpret_cast<const f32x4 *>(&lds.top[buffer][sub * kSubBlocks]);
         if (__builtin_amdgcn_readfirstlane(min(min(valid[0], valid[1]), min(valid[2], valid[3]))) < 16 || token + kSub > least) {
             // what lies past the end of the keys, or of what a row sees, counts nothing (the scales there are zero already)
+            int at = 4 * g4;
+            asm volatile("" : "+v"(at));                   // keeps all of it behind its branch: whole steps pay nothing
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int at = 4 * g4 + (i & 3);
+            for (int b = 0; b < kSubBlocks; ++b)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const int end = min(valid[i >> 2], r[t].seen - token - 16 * (i >> 2));
-                    x[t][i] = at < end ? x[t][i] : -__builtin_inff();
+                    const int left = min(valid[b], r[t].seen - token - 16 * b) - at;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][4 * b + i] = i < left ? x[t][4 * b + i] : -__builtin_inff();
                 }
-            }
-            asm volatile("" ::: );                       // stays a branch: the whole steps pay nothing
         }
         const float shrink = ref.raise(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
         f16x8 prob[NT][N / 8][TERMS];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) probabilities<D, TERMS, N>(st[t], x[t], sv, r[t].factor, ref, shrink, prob[t]);
+        for (int t = 0; t < NT; ++t) {
+            raise_maximum<D, N>(st[t], x[t], r[t].factor, ref, shrink);
+            probabilities<D, TERMS, N>(st[t], x[t], sv, r[t].factor, prob[t]);
+        }
 #pragma unroll
         for (int c = 0; c < N / 8; ++c)
 #pragma unroll
