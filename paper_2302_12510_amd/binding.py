@@ -110,9 +110,11 @@ class _Ctypes:
     def dybit_packed_bytes(self, pair, n):
         return int(lib().dybit_packed_bytes(fmt(*pair), n))
 
-    def dybit_head_norm_rope(self, q, k, q_weight, k_weight, positions, cos, sin, rows, rotary, neighbours, eps, q_out, k_out, stream):
+    def head_norm_rope(self, q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours, out, stream):
+        _check_rotation(q, q_weight, k, k_weight, positions, cos, sin)
+        q_out, k_out = out if out is not None else (self.empty_rows(q), None if k is None else self.empty_rows(k))
         return lib().dybit_head_norm_rope(_heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _typed(positions, torch.int64), _ptr(cos), _ptr(sin),
-                                          rows, rotary, neighbours, eps, _heads(q_out), _heads(k_out), _stream(stream))
+                                          cos.shape[0], 2 * cos.shape[1], bool(neighbours), eps, _heads(q_out), _heads(k_out), _stream(stream)), q_out, k_out
 
     def dybit_head_norm_rope_bwd(self, gq, gk, q, k, q_weight, k_weight, positions, cos, sin, rows, rotary, neighbours, eps, dq, dk, dwq, dwk, work,
                                  stream):
@@ -733,19 +735,18 @@ def dybit_head_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight: torc
     heads) and the rotation by positions (int64 [tokens]) of its first 2 * cos.shape[1] elements; cos, sin: float32 [positions]
     [pairs].  neighbours: pairs are neighbouring elements, not halves.  out: (q_out, k_out), which may be (q, k).
     Returns (q_out, k_out)."""
-    q_out, k_out = out if out is not None else (_n().empty_rows(q), None if k is None else _n().empty_rows(k))
-    _check_rotation(q, q_weight, k, k_weight, positions, cos, sin)
-    _check(_n().dybit_head_norm_rope(q, k, q_weight, k_weight, positions, cos, sin, cos.shape[0], 2 * cos.shape[1], bool(neighbours), eps,
-                                     q_out, k_out, stream), "dybit_head_norm_rope")
+    status, q_out, k_out = _n().head_norm_rope(q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours, out, stream)
+    _check(status, "dybit_head_norm_rope")
     return q_out, k_out
 
 
 def _check_rotation(q, q_weight, k, k_weight, positions, cos, sin):
-    assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and q_weight.dtype == torch.float32
+    if any(t.dtype != torch.float32 for t in (cos, sin, q_weight)) or k is not None and k_weight.dtype != torch.float32:
+        raise TypeError("expected a tensor of float32")
     if cos.dim() != 2 or cos.shape != sin.shape or positions.shape != q.shape[:1] or q_weight.numel() != q.shape[-1]:
         raise ValueError("expected tables [positions][pairs], a position a token and a weight an element of a head")
-    if k is not None and (k_weight.dtype != torch.float32 or k_weight.numel() != k.shape[-1]):
-        raise ValueError("expected a float32 weight for every element of a key head")
+    if k is not None and k_weight.numel() != k.shape[-1]:
+        raise ValueError("expected a weight for every element of a key head")
 
 
 def dybit_head_norm_rope_bwd(grad_q: torch.Tensor, grad_k: torch.Tensor | None, q: torch.Tensor, k: torch.Tensor | None, q_weight: torch.Tensor,

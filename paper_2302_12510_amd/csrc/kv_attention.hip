@@ -47,7 +47,8 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4;
     const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
-    const int row0 = (int)blockIdx.y * (16 * NT), slot = blockIdx.z;
+    const int row0 = (int)blockIdx.y * (16 * NT);
+    const int slot = (int)(gridDim.z - 1 - blockIdx.z);      // ends of long sequences first, the short ones, which fill the gaps, with the last
     const Segment g = segment(p, seg);
     if (g.odd && head == 0 && blockIdx.y == 0 && slot == 0 && threadIdx.x == 0) *p.err = DYBIT_ERR_INVALID_ARG;
     if (row0 >= g.count * p.group) return;

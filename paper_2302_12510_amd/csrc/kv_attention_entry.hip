@@ -19,7 +19,7 @@ constexpr int kThreads = 256, kWaves = 4;
 // partial results (4 (D + 2) bytes a row, written and read back); but no longer ones than kLongest for few rows, which keeps batches of
 // very different lengths even.
 constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
-constexpr int32_t kShortest = 128, kLongest = 2048;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
+constexpr int32_t kShortest = 128, kLongest = 1536;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
 // fp32 is split into two halves.
 int terms_of(int type) { return type == DYBIT_F32 ? 2 : 1; }
