@@ -45,7 +45,7 @@ struct Vals {
 template <int D, int TERMS, int NT>
 __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
     const int row0 = (int)blockIdx.y * (16 * NT);
     const int slot = (int)(gridDim.z - 1 - blockIdx.z);      // ends of long sequences first, the short ones, which fill the gaps, with the last
