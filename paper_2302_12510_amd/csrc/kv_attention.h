@@ -5,6 +5,8 @@
 namespace dybit {
 namespace kv {
 
+struct Left;
+
 // One phase of an attention call: queries over the tokens that each segment (a sequence's own pages, or a group's prefix) holds.
 struct Phase {
     const void *q;
@@ -20,8 +22,10 @@ struct Phase {
     int64_t max_queries, cap;                          // cap: most tokens of a segment that are looked at
     int32_t causal, chunk;                             // chunk: tokens of a segment that one workgroup goes through
     float scale;                                       // times log2(e)
+    Left *left;                                        // whole: kCus of them
     float *part_out, *part_stat;                       // partial results [token][query head][slot][D], (maximum, sum); NULL: write out
     int64_t slot0, slots;                              // first slot of the phase; slots of a row
+    int32_t whole;                                     // wide kernel: tiles of rows go to workgroups whole, but the last ones in parts (Tile)
     int *err;
 };
 
@@ -67,12 +71,85 @@ __device__ __forceinline__ int visible(const Phase &p, const Segment &g, int i)
     return n < 0 ? 0 : n;
 }
 
+// Tiles of rows that go to workgroups whole (Phase::whole).  The tiles of all segments, the last of a segment first, and of all key
+// heads, heads next to each other, fill the device's kCus workgroups some number of times; those left over, fewer than kCus, are cut
+// along the keys into as many parts as give all workgroups one (none, where they are more than half; kMostParts at most), so that the
+// last turn is a short one too.  Which
+// they are depends on the segments' numbers of queries, so workgroups find their tile themselves and leave word of it for the join.
+// Parts lie at [left-over tile][kMostParts][row of the tile].
+constexpr int kCus = 256, kMostParts = 8;
+struct Left { int seg, head, tile, parts; };           // a left-over tile, for the join; the last one of kCus: how many there are (seg)
+struct Tile {
+    int seg, head, tile;
+    int part, parts;                                   // parts 0: whole
+    int left, lefts;                                   // which left-over tile, of how many
+    bool real;
+};
+constexpr int64_t kLeftBytes = kCus * sizeof(Left);    // in front of the parts
+
+// Tile of workgroup `block`.  All lanes of a wave call it, with the same arguments.
+__device__ __forceinline__ Tile find_tile(const Phase &p, int rows, int block, int lane)
+{
+    int total = 0, mine = 0;
+    auto tiles_of = [&](int s) {
+        if (s >= p.sequences) return 0;
+        const Segment g = segment(p, s);
+        if (g.odd && block == 0) *p.err = DYBIT_ERR_INVALID_ARG;
+        return (g.count * p.group + rows - 1) / rows;
+    };
+    for (int s = 0; s < p.sequences; s += 64) {
+        mine = tiles_of(s + lane);
+        int sum = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+        total += sum;
+    }
+    total = __builtin_amdgcn_readfirstlane(total) * p.kv_heads;
+    const int whole = total / kCus * kCus, left = total - whole;
+    const int stride = (left + 7) & ~7;                    // parts of a tile on the same chiplet
+    const int parts = left ? min(kCus / stride, kMostParts) : 0;
+    Tile t;
+    int u = block;
+    t.part = t.parts = 0;
+    t.lefts = parts > 1 ? left : 0;
+    if (parts > 1 && block >= whole) {
+        t.parts = parts;
+        t.part = (block - whole) / stride;
+        u = whole + (block - whole) - t.part * stride;
+    }
+    t.left = u - whole;
+    t.real = u < total && (t.parts == 0 || t.part < t.parts);
+    const int v = u / p.kv_heads;
+    t.head = u - v * p.kv_heads;
+    t.seg = t.tile = 0;
+    int before = 0;
+    for (int s = 0; t.real && s < p.sequences; s += 64) {
+        if (p.sequences > 64) mine = tiles_of(s + lane);
+        int upto = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int y = __shfl_up(upto, off);
+            if (lane >= off) upto += y;
+        }
+        const unsigned long long found = __ballot(before + upto > v);
+        if (found) {
+            const int at = __builtin_ctzll(found);
+            t.seg = s + at;
+            t.tile = before + __builtin_amdgcn_readlane(upto, at) - 1 - v;       // the last tile of a segment first
+            break;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return t;
+}
+
 // How a phase is run: decided on the host from sizes alone.
 struct Plan {
     bool wide;                                         // kv_attention_wide.hip, else kv_attention.hip
     int32_t tiles16;                                   // 16-row tiles of a wave of the latter: 1 or 2
+    bool whole;                                        // Phase::whole
     int32_t chunk;
-    int64_t row_tiles, slots;
+    int64_t row_tiles, slots, tiles;                   // tiles: at most so many, of all segments and key heads
 };
 
 void launch_k8v8(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);

@@ -173,11 +173,11 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
         const Values<VB, D / 16> values(vals.w);
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
-            const f16x8 a = values.dim(j);
+            const f16x8 a = values.dim(j), first = TERMS == 2 ? times_rest(a) : a;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][0][e], st[t].o[j], 0, 0, 0);
+                for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e ? a : first, prob[t][0][e], st[t].o[j], 0, 0, 0);
         }
         if constexpr (decltype(more)::value) fetch_values(vals, step + kWaves);
     };
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
     // join the four waves: 2 and 3 into 0 and 1, then 1 into 0
     __shared__ float s_m[2][NT][16], s_l[2][NT][16], s_o[2][NT][D / 4][64];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) settle<VB>(st[t], r[t].factor, ref);
+    for (int t = 0; t < NT; ++t) settle<VB, TERMS>(st[t], r[t].factor, ref);
 #pragma unroll
     for (int half = 2; half >= 1; half >>= 1) {
         if (wave >= half && wave < 2 * half) {
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (r[t].row < 0) continue;
-        write_row<D>(p, r[t].row, slot, g4, st[t]);
+        write_row<D>(p, r[t].row, p.part_out ? r[t].row * p.slots + p.slot0 + slot : -1, g4, st[t]);
     }
 }
 

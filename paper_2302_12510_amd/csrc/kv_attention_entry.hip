@@ -17,14 +17,15 @@ constexpr int kThreads = 256, kWaves = 4;
 // whose waves share the rows out.  The tokens of a segment go to workgroups in chunks: as many as the device holds workgroups at once
 // (kHeld, by the kernels' registers), were all segments as long as the longest, since fewer leave it idle and more add their start and their
 // partial results (4 (D + 2) bytes a row, written and read back); but no longer ones than kLongest for few rows, which keeps batches of
-// very different lengths even.
+// very different lengths even.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be joined with
+// them), they go whole, but for the last ones (Tile).
 constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
 constexpr int32_t kShortest = 128, kLongest = 1536;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
 // fp32 is split into two halves.
 int terms_of(int type) { return type == DYBIT_F32 ? 2 : 1; }
 
-Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, int64_t cap)
+Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, int64_t cap, int64_t all_rows, bool may_be_whole)
 {
     Plan p{};
     p.wide = max_rows > 32;
@@ -37,12 +38,23 @@ Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, 
     int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
     chunk = std::max<int64_t>(chunk, kShortest);
     if (!p.wide) chunk = std::min<int64_t>(chunk, kLongest);
+    // a segment's last tile may be part full: no more tiles than full ones of all rows there are and one a segment
+    p.tiles = std::min(segments * p.row_tiles, all_rows / rows + segments) * kv_heads;
+    p.whole = may_be_whole && p.wide && p.tiles >= kCus;
+    if (p.whole) chunk = 0x7fffff00;
     p.chunk = (int32_t)chunk;
     p.slots = std::max<int64_t>(1, (cap + chunk - 1) / chunk);
     return p;
 }
 
 struct Split {
+    // parts of rows in the workspace
+    size_t parts(const dybit_heads &q) const
+    {
+        if (own.whole) return (size_t)(kCus - 1) * kMostParts * (size_t)(kWideRows * wide_waves(q.head_dim, terms_of(q.type)));
+        return (size_t)slots * (size_t)q.tokens * (size_t)q.heads;
+    }
+    size_t bytes(const dybit_heads &q) const { return parts(q) * (size_t)(q.head_dim + 2) * 4 + (own.whole ? (size_t)kLeftBytes : 0); }
     Plan own, prefix;
     int64_t own_cap, prefix_cap, slots;                   // slots: 0 where workgroups write the results themselves
 };
@@ -60,10 +72,10 @@ Split split_of(const dybit_heads &q, const dybit_kv_cache &c, int64_t width, int
     Split s{};
     const int group = q.heads / c.heads;
     s.own_cap = cap_of(c, width, max_length);
-    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, q.type, s.own_cap);
+    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, q.type, s.own_cap, q.tokens * group, prefix.groups == 0);
     if (prefix.groups) {
         s.prefix_cap = cap_of(c, prefix.table_width, prefix.max_length);
-        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, q.type, s.prefix_cap);
+        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, q.type, s.prefix_cap, q.tokens * group, false);
         s.slots = s.own.slots + s.prefix.slots;
     } else {
         s.slots = s.own.slots > 1 ? s.own.slots : 0;
@@ -208,6 +220,61 @@ void join(const Join &j, int D, int64_t max_queries, int64_t sequences, hipStrea
 #undef DYBIT_JOIN
 }
 
+// The parts of the tiles that were left over: a workgroup has 16 rows of one, a wave four.
+template <int D>
+__global__ __launch_bounds__(kThreads) void join_left_kernel(const Phase p, int rows)
+{
+    constexpr int N = D / 64, MINE = 4;
+    const int lane = threadIdx.x & 63, per_tile = rows / (kWaves * MINE), at = (int)(blockIdx.x / (unsigned)per_tile);
+    if (at >= p.left[kCus - 1].seg) return;
+    const Left tile = p.left[at];
+    const Segment g = segment(p, tile.seg);
+    const int first = (int)(blockIdx.x % (unsigned)per_tile) * (kWaves * MINE) + (int)(threadIdx.x >> 6) * MINE;
+#pragma unroll 1
+    for (int r = 0; r < MINE; ++r) {
+        const int n = tile.tile * rows + first + r, i = (int)((unsigned)n / (unsigned)p.group);
+        if (i >= g.count) return;
+        float2 stat[kMostParts];
+        float x[kMostParts][N], m = -__builtin_inff(), l = 0.0f, y[N];
+#pragma unroll
+        for (int k = 0; k < kMostParts; ++k) {
+            const int64_t row = ((int64_t)at * kMostParts + k) * rows + first + r;
+            stat[k] = float2{-__builtin_inff(), 0.0f};
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[k][j] = 0.0f;
+            if (k < tile.parts) {
+                stat[k] = *reinterpret_cast<const float2 *>(p.part_stat + 2 * row);
+                heads::Pack<float, N>::load(p.part_out + row * D + N * lane, x[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kMostParts; ++k) m = fmaxf(m, stat[k].x);
+        const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[j] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kMostParts; ++k) {
+            const float w = __builtin_amdgcn_exp2f(stat[k].x - base);
+            l += w * stat[k].y;
+#pragma unroll
+            for (int j = 0; j < N; ++j) y[j] += w * x[k][j];
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const int64_t to = (g.first + i) * p.out_token + (tile.head * p.group + n - i * p.group) * p.out_head + N * lane;
+#pragma unroll
+        for (int j = 0; j < N; ++j) store_one(p, to + j, y[j] * inv);
+    }
+}
+
+void join_left(const Phase &p, int D, hipStream_t st)
+{
+    const int rows = kWideRows * wide_waves(D, terms_of(p.type));
+    const dim3 grid((unsigned)((kCus - 1) * (rows / 16))), block(kThreads);
+    if (D == 64) hipLaunchKernelGGL(join_left_kernel<64>, grid, block, 0, st, p, rows);
+    else if (D == 128) hipLaunchKernelGGL(join_left_kernel<128>, grid, block, 0, st, p, rows);
+    else hipLaunchKernelGGL(join_left_kernel<256>, grid, block, 0, st, p, rows);
+}
+
 void launch(const Phase &p, const Plan &plan, const dybit_kv_cache &c, int64_t segments, hipStream_t st)
 {
     const int terms = terms_of(p.type);
@@ -228,7 +295,7 @@ extern "C" size_t dybit_kv_attention_workspace_bytes(dybit_heads q, dybit_kv_cac
     if (kv::check_sizes(q, cache, table_width, sequences, max_queries, max_length, prefix) != DYBIT_OK) return 0;
     if (q.tokens == 0 || sequences == 0) return 0;
     const kv::Split s = kv::split_of(q, cache, table_width, sequences, max_queries, max_length, prefix);
-    return (size_t)s.slots * (size_t)q.tokens * (size_t)q.heads * (size_t)(q.head_dim + 2) * 4;
+    return s.bytes(q);
 }
 
 extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, const int32_t *tables, int64_t table_width, const int32_t *lengths,
@@ -248,8 +315,7 @@ extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, 
     const kv::Split s = kv::split_of(q, cache, table_width, sequences, max_queries, max_length, prefix);
     // grids: y (row tiles; sequences in the join) and z (chunks) stay under 2^16
     if (s.own.row_tiles > 65535 || s.own.slots > 65535 || s.prefix.row_tiles > 65535 || s.prefix.slots > 65535) return DYBIT_ERR_INVALID_ARG;
-    const int64_t rows = q.tokens * q.heads;
-    const size_t need = (size_t)s.slots * (size_t)rows * (size_t)(q.head_dim + 2) * 4;
+    const size_t need = s.bytes(q);
     if (need > workspace_bytes) return DYBIT_ERR_INVALID_ARG;
     if (need && !workspace) return DYBIT_ERR_NULL;
     if (need && !aligned16(workspace)) return DYBIT_ERR_ALIGNMENT;
@@ -263,15 +329,18 @@ extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, 
     p.kv_heads = cache.heads; p.group = q.heads / cache.heads; p.page_shift = kv::log2_of(cache.page_tokens);
     p.starts = starts; p.tokens = q.tokens; p.sequences = sequences;
     p.scale = scale * 1.44269504088896340736f;
-    p.part_out = need ? (float *)workspace : nullptr;
-    p.part_stat = need ? (float *)workspace + (size_t)s.slots * (size_t)rows * (size_t)q.head_dim : nullptr;
+    if (need) {
+        if (s.own.whole) p.left = (kv::Left *)workspace;
+        p.part_out = (float *)(workspace + (s.own.whole ? kv::kLeftBytes : 0));
+        p.part_stat = p.part_out + s.parts(q) * (size_t)q.head_dim;
+    }
     p.slots = s.slots;
     p.err = async_error_word();
     if (!p.err) return DYBIT_ERR_HIP;
     kv::Join j{};
     j.own = p;
     j.own.tables = tables; j.own.lengths = lengths; j.own.table_width = table_width; j.own.max_queries = max_queries; j.own.cap = s.own_cap;
-    j.own.causal = causal; j.own.chunk = s.own.chunk; j.own.slot0 = prefix.groups ? s.prefix.slots : 0;
+    j.own.whole = s.own.whole; j.own.causal = causal; j.own.chunk = s.own.chunk; j.own.slot0 = prefix.groups ? s.prefix.slots : 0;
     j.own_slots = (int32_t)s.own.slots;
     if (prefix.groups) {
         j.prefix = p;
@@ -282,6 +351,7 @@ extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, 
         kv::launch(j.prefix, s.prefix, cache, prefix.groups, hs);
     }
     kv::launch(j.own, s.own, cache, sequences, hs);
-    if (need) kv::join(j, cache.head_dim, max_queries, sequences, hs);
+    if (s.own.whole) kv::join_left(j.own, cache.head_dim, hs);
+    else if (need) kv::join(j, cache.head_dim, max_queries, sequences, hs);
     return launch_status();
 }

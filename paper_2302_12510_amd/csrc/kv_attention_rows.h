@@ -185,7 +185,7 @@ __device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const
         u32 w[TERMS][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if constexpr (TERMS == 2) split_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], w[0][i], w[1][i]);
+            if constexpr (TERMS == 2) split_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], w[0][i], w[1][i], kRest);
             else w[0][i] = round_pair(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
         }
 #pragma unroll
@@ -194,24 +194,23 @@ __device__ __forceinline__ void probabilities(State<D> &st, float (&x)[N], const
 }
 
 // The state in units of its own: over all lanes of a row, without the reference and the fold of the codes.
-template <int VB, int D>
+template <int VB, int TERMS, int D>
 __device__ __forceinline__ void settle(State<D> &st, float factor, const Reference &ref)
 {
     st.l += __shfl_xor(st.l, 16);
     st.l += __shfl_xor(st.l, 32);
     st.l *= ref.value();
     st.m *= factor;
-    const float back = ref.value() * fold<VB>();
+    const float back = ref.value() * (TERMS == 2 ? fold<VB>() / kRest : fold<VB>());
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) st.o[j] *= back;
 }
 
-// A row's result, or its part of one: a lane has dims (D / 16) (4 g4 + i) + j of its row.
+// A row's result, or (at >= 0) its part of one: a lane has dims (D / 16) (4 g4 + i) + j of its row.
 template <int D>
-__device__ __forceinline__ void write_row(const Phase &p, int64_t row, int slot, int g4, const State<D> &st)
+__device__ __forceinline__ void write_row(const Phase &p, int64_t row, int64_t at, int g4, const State<D> &st)
 {
-    if (p.part_out) {
-        const int64_t at = row * p.slots + p.slot0 + slot;
+    if (at >= 0) {
         if (g4 == 0) *reinterpret_cast<float2 *>(p.part_stat + 2 * at) = float2{st.m, st.l};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -223,14 +222,14 @@ __device__ __forceinline__ void write_row(const Phase &p, int64_t row, int slot,
     } else {
         const int heads_q = p.kv_heads * p.group;
         const int64_t token = row / heads_q;
-        const int64_t at = token * p.out_token + (row - token * heads_q) * p.out_head;
+        const int64_t to = token * p.out_token + (row - token * heads_q) * p.out_head;
         const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;                  // a row that sees nothing: zeros
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float x[D / 16];
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) x[j] = st.o[j][i] * inv;
-            store_result<D / 16>(p, at + (D / 16) * (4 * g4 + i), x);
+            store_result<D / 16>(p, to + (D / 16) * (4 * g4 + i), x);
         }
     }
 }

@@ -50,17 +50,38 @@ __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4
     constexpr int BUFFERS = D == 256 ? 1 : 2;            // 64 KB a step of 256 dims
     __shared__ Lds<D, WAVES, BUFFERS> lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
-    const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
-    const int row0 = (int)(gridDim.y - 1 - blockIdx.y) * (16 * NT * WAVES);        // causal: those with the most keys first
-    const int slot = blockIdx.z;
+    constexpr int ROWS = 16 * NT * WAVES;
+    int seg, head, row0, slot = 0;
+    Tile tile;
+    tile.parts = 0;
+    if (p.whole) {
+        tile = find_tile(p, ROWS, (int)blockIdx.x, lane);
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.left[kCus - 1].seg = tile.lefts;
+        if (!tile.real) return;
+        seg = tile.seg;
+        head = tile.head;
+        row0 = tile.tile * ROWS;
+    } else {
+        seg = (int)(blockIdx.x / (unsigned)p.kv_heads);
+        head = (int)blockIdx.x - seg * p.kv_heads;
+        row0 = (int)(gridDim.y - 1 - blockIdx.y) * ROWS;   // causal: those with the most keys first
+        slot = blockIdx.z;
+    }
     const Segment g = segment(p, seg);
     if (g.odd && head == 0 && row0 == 0 && slot == 0 && threadIdx.x == 0) *p.err = DYBIT_ERR_INVALID_ARG;
     if (row0 >= g.count * p.group) return;
-    int last = (int)((unsigned)(row0 + 16 * NT * WAVES - 1) / (unsigned)p.group);
+    int last = (int)((unsigned)(row0 + ROWS - 1) / (unsigned)p.group);
     last = last < g.count ? last : g.count - 1;
-    const int lo = slot * p.chunk, most = visible(p, g, last);
-    const int hi = most - lo < p.chunk ? most : lo + p.chunk;
-    if (lo >= hi && p.part_out) return;
+    const int most = visible(p, g, last);
+    int lo = slot * p.chunk, hi = most - lo < p.chunk ? most : lo + p.chunk;
+    if (tile.parts) {
+        const int all = (most + STEP - 1) / STEP, each = (all + tile.parts - 1) / tile.parts * STEP;
+        lo = tile.part * each;
+        hi = most - lo < each ? most : lo + each;
+        if (tile.part == 0 && threadIdx.x == 0) p.left[tile.left] = Left{seg, head, tile.tile, each ? (most + each - 1) / each : 0};
+    }
+    const bool parted = p.whole ? tile.parts > 0 : p.part_out != nullptr;
+    if (lo >= hi && parted) return;
 
     const int steps = (hi - lo + STEP - 1) / STEP;
     const int32_t *table = p.tables + (int64_t)seg * p.table_width;
@@ -184,16 +205,13 @@ __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4
         for (int c = 0; c < N / 8; ++c)
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
-                const f16x8 a = lds.v[buffer][sub * (N / 8) + c][j][lane];
+                const f16x8 a = lds.v[buffer][sub * (N / 8) + c][j][lane], first = TERMS == 2 ? times_rest(a) : a;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, prob[t][c][e], st[t].o[j], 0, 0, 0);
+                    for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e ? a : first, prob[t][c][e], st[t].o[j], 0, 0, 0);
             }
     };
-    // Half of the waves decode the next step before this one's products and half behind them: while some of a SIMD's waves use the
-    // vector unit, the others use the matrix unit.
-    const bool early = wave >= WAVES / 2;
     auto prepare = [&](int step) {                       // codes of `step` are in registers
         if (step < steps) decode(share, step & (BUFFERS - 1));
         if (step + 1 < steps) fetch(share, step + 1);
@@ -202,29 +220,31 @@ __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4
     __syncthreads();
     for (int step = 0; step < steps; ++step) {
         const int buffer = step & (BUFFERS - 1), token = lo + step * STEP;
-        if (BUFFERS == 2 && early) prepare(step + 1);
         if (works) {
 #pragma unroll 1
             for (int sub = 0; sub < STEP / kSub; ++sub)
                 if (token + sub * kSub < hi) go(token + sub * kSub, buffer, sub);
         }
         if (BUFFERS == 1) __syncthreads();
-        if (BUFFERS == 1 || !early) prepare(step + 1);
+        prepare(step + 1);
         __syncthreads();
     }
 
     if (!works) return;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        settle<VB>(st[t], r[t].factor, ref);
-        if (r[t].row >= 0) write_row<D>(p, r[t].row, slot, g4, st[t]);
+        settle<VB, TERMS>(st[t], r[t].factor, ref);
+        if (r[t].row < 0) continue;
+        const int64_t at = p.whole ? ((int64_t)tile.left * kMostParts + tile.part) * ROWS + 16 * (NT * wave + t) + (lane & 15) : r[t].row * p.slots + p.slot0 + slot;
+        write_row<D>(p, r[t].row, parted ? at : -1, g4, st[t]);
     }
 }
 
 template <int D>
 void launch_d(const Phase &p, const Plan &plan, int terms, int64_t segments, hipStream_t st)
 {
-    const dim3 grid((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots), block((unsigned)(64 * wide_waves(D, terms)));
+    const dim3 grid = plan.whole ? dim3((unsigned)(plan.tiles + kCus)) : dim3((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots);
+    const dim3 block((unsigned)(64 * wide_waves(D, terms)));
     if (terms == 1) hipLaunchKernelGGL((attention_wide_kernel<D, 1>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((attention_wide_kernel<D, 2>), grid, block, 0, st, p);
 }

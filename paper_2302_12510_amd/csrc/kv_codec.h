@@ -108,13 +108,18 @@ template <int DIMS> struct Values<4, DIMS> {
 // rounds a product to fp16 here in one step and there in two, and the rest would belong to another half than the one that is used.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u32 round_pair(float a, float b) { return __builtin_bit_cast(u32, __builtin_convertvector((f32x2{a, b}), f16x2)); }
-__device__ __forceinline__ void split_pair(float a, float b, u32 &high, u32 &low)
+__device__ __forceinline__ void split_pair(float a, float b, u32 &high, u32 &low, float times = 1.0f)
 {
     high = round_pair(a, b);
     asm("" : "+v"(high));
     const f16x2 h = __builtin_bit_cast(f16x2, high);
-    low = round_pair(a - (float)h[0], b - (float)h[1]);
+    low = round_pair((a - (float)h[0]) * times, (b - (float)h[1]) * times);
 }
+
+// The rest of a split probability is taken 2^10-fold, and the values for its first half too (exact: they are within 2^-20 and 2^12
+// then), so that the rests of small probabilities are not lost below the smallest half.
+constexpr float kRest = 1024.0f;
+__device__ __forceinline__ f16x8 times_rest(f16x8 a) { return a * (f16x8)((_Float16)kRest); }
 
 // BYTES (1, 2, 4, 8, 16, 32, 64) from p into whole words.
 template <int BYTES>

@@ -50,6 +50,17 @@ def test_chunks_of_a_prompt(n, dtype):
     check_attention(rng, World(rng, [n, n + 77, 2 * n + 1], 1, 128, (8, 8), 32), [n, n, n - 30], 3, dtype)
 
 
+@pytest.mark.parametrize("D,dtype", [(64, "fp16"), (64, "fp32"), (128, "bf16"), (256, "fp16")])
+@pytest.mark.parametrize("sequences,heads,n", [(32, 8, 20), (70, 4, 18), (5, 16, 150), (33, 9, 17)])
+def test_more_tiles_of_rows_than_the_device_holds(D, dtype, sequences, heads, n):
+    """Tiles are shared out whole but for the last ones, which are cut along the keys; which ones the numbers of queries say."""
+    rng = np.random.default_rng(sequences + D)
+    new = [int(x) for x in rng.integers(0, n + 1, sequences)]
+    new[sequences // 2] = n
+    lengths = [max(0, c + int(rng.integers(-3, 60))) if i % 5 else int(rng.integers(0, 300)) for i, c in enumerate(new)]
+    check_attention(rng, World(rng, lengths, heads, D, (8, 4), 16), new, 2 * heads, dtype)
+
+
 @pytest.mark.parametrize("D,bits,dtype", [(64, (4, 4), "fp16"), (128, (8, 8), "bf16"), (128, (4, 8), "fp32"), (256, (8, 4), "bf16")])
 @pytest.mark.parametrize("new", [None, [1, 3, 0, 2, 30, 4, 1]])
 def test_shared_prefix(D, bits, dtype, new):
