@@ -7,6 +7,13 @@ namespace kv {
 
 struct Left;
 
+// A shared prefix as those see it that join its parts with a sequence's own tokens.
+struct Shared {
+    const int32_t *lengths, *members;                  // members: first sequence of each group
+    int64_t max_queries, cap;
+    int32_t groups, chunk;                             // groups 0: no prefix
+};
+
 // One phase of an attention call: queries over the tokens that each segment (a sequence's own pages, or a group's prefix) holds.
 struct Phase {
     const void *q;
@@ -22,6 +29,7 @@ struct Phase {
     int64_t max_queries, cap;                          // cap: most tokens of a segment that are looked at
     int32_t causal, chunk;                             // chunk: tokens of a segment that one workgroup goes through
     float scale;                                       // times log2(e)
+    Shared shared;                                     // groups > 0: the prefix' parts are joined here (kv_attention.hip)
     Left *left;                                        // whole: kCus of them
     float *part_out, *part_stat;                       // partial results [token][query head][slot][D], (maximum, sum); NULL: write out
     int64_t slot0, slots;                              // first slot of the phase; slots of a row
@@ -62,6 +70,24 @@ __device__ __forceinline__ Segment segment(const Phase &p, int s)
     g.odd |= n < 0 || n > p.cap;
     g.length = (int32_t)(n < 0 ? 0 : n > p.cap ? p.cap : n);
     return g;
+}
+
+// Parts that the prefix has left for a sequence's query token `token` (0: it has none): those of the group that names it.
+__device__ __forceinline__ int parts_before(const Phase &p, const Shared &x, int seq, int64_t token)
+{
+    int a = 0, b = x.groups;
+    while (b - a > 1) {
+        const int mid = (a + b) >> 1;
+        if (x.members[mid] <= seq) a = mid; else b = mid;
+    }
+    if (!x.groups || x.members[a] > seq || seq >= x.members[a + 1]) return 0;
+    Phase whole = p;
+    whole.members = x.members;
+    whole.lengths = x.lengths;
+    whole.max_queries = x.max_queries;
+    whole.cap = x.cap;
+    const Segment g = segment(whole, a);
+    return token >= g.first && token < g.first + g.count ? (g.length + x.chunk - 1) / x.chunk : 0;
 }
 
 // Keys that query i of a segment sees.

@@ -57,7 +57,8 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
     last = last < g.count ? last : g.count - 1;
     const int lo = slot * p.chunk, most = visible(p, g, last);
     const int hi = most - lo < p.chunk ? most : lo + p.chunk;
-    if (lo >= hi && p.part_out) return;
+    const bool joins = p.shared.groups > 0, parted = p.part_out && !joins;
+    if (lo >= hi && parted) return;
 
     // the pages of this wave's blocks of 16 tokens, one a lane: block j is step wave + 4 (j / 2), half j % 2
     const int steps = (hi - lo + 31) >> 5;
@@ -191,6 +192,40 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
     __shared__ float s_m[2][NT][16], s_l[2][NT][16], s_o[2][NT][D / 4][64];
 #pragma unroll
     for (int t = 0; t < NT; ++t) settle<VB, TERMS>(st[t], r[t].factor, ref);
+    if (joins) {
+        // the prefix' parts of these rows, shared out over the waves, two at a time
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int heads_q = p.kv_heads * p.group;
+            const int parts = r[t].row >= 0 ? parts_before(p, p.shared, seg, r[t].row / heads_q) : 0;
+            for (int k = wave; __any(k < parts); k += 2 * kWaves) {
+                float2 stat[2];
+                float x[2][4][D / 16];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    stat[b] = float2{-__builtin_inff(), 0.0f};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j) x[b][i][j] = 0.0f;
+                    if (k + b * kWaves < parts) {
+                        const int64_t at = r[t].row * p.slots + k + b * kWaves;
+                        stat[b] = *reinterpret_cast<const float2 *>(p.part_stat + 2 * at);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) heads::Pack<float, D / 16>::load(p.part_out + at * D + (D / 16) * (4 * g4 + i), x[b][i]);
+                    }
+                }
+                const float m = fmaxf(st[t].m, fmaxf(stat[0].x, stat[1].x)), base = m == -__builtin_inff() ? 0.0f : m;
+                const float a = __builtin_amdgcn_exp2f(st[t].m - base), w0 = __builtin_amdgcn_exp2f(stat[0].x - base), w1 = __builtin_amdgcn_exp2f(stat[1].x - base);
+                st[t].m = m;
+                st[t].l = st[t].l * a + stat[0].y * w0 + stat[1].y * w1;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) st[t].o[j][i] = st[t].o[j][i] * a + x[0][i][j] * w0 + x[1][i][j] * w1;
+            }
+        }
+    }
 #pragma unroll
     for (int half = 2; half >= 1; half >>= 1) {
         if (wave >= half && wave < 2 * half) {
@@ -223,7 +258,7 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (r[t].row < 0) continue;
-        write_row<D>(p, r[t].row, p.part_out ? r[t].row * p.slots + p.slot0 + slot : -1, g4, st[t]);
+        write_row<D>(p, r[t].row, parted ? r[t].row * p.slots + p.slot0 + slot : -1, g4, st[t]);
     }
 }
 

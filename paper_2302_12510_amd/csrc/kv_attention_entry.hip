@@ -17,15 +17,16 @@ constexpr int kThreads = 256, kWaves = 4;
 // whose waves share the rows out.  The tokens of a segment go to workgroups in chunks: as many as the device holds workgroups at once
 // (kHeld, by the kernels' registers), were all segments as long as the longest, since fewer leave it idle and more add their start and their
 // partial results (4 (D + 2) bytes a row, written and read back); but no longer ones than kLongest for few rows, which keeps batches of
-// very different lengths even.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be joined with
+// very different lengths even; twice as many behind a prefix, where there is a join anyway.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be joined with
 // them), they go whole, but for the last ones (Tile).
 constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
+constexpr int32_t kJoined = 512;                           // tokens behind a prefix that one workgroup joins with it
 constexpr int32_t kShortest = 128, kLongest = 1536;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
 // fp32 is split into two halves.
 int terms_of(int type) { return type == DYBIT_F32 ? 2 : 1; }
 
-Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, int64_t cap, int64_t all_rows, bool may_be_whole)
+Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, int64_t cap, int64_t all_rows, bool behind, bool may_be_whole)
 {
     Plan p{};
     p.wide = max_rows > 32;
@@ -34,7 +35,7 @@ Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, 
     const int64_t rows = p.wide ? kWideRows * waves : 16 * p.tiles16;
     p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
     const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
-    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide / waves : kHeld) / base);
+    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide / waves : behind ? 2 * kHeld : kHeld) / base);
     int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
     chunk = std::max<int64_t>(chunk, kShortest);
     if (!p.wide) chunk = std::min<int64_t>(chunk, kLongest);
@@ -57,6 +58,7 @@ struct Split {
     size_t bytes(const dybit_heads &q) const { return parts(q) * (size_t)(q.head_dim + 2) * 4 + (own.whole ? (size_t)kLeftBytes : 0); }
     Plan own, prefix;
     int64_t own_cap, prefix_cap, slots;                   // slots: 0 where workgroups write the results themselves
+    bool joins;                                           // the prefix' parts are joined by the workgroups of the own tokens
 };
 
 int64_t cap_of(const dybit_kv_cache &c, int64_t width, int64_t max_length)
@@ -72,11 +74,18 @@ Split split_of(const dybit_heads &q, const dybit_kv_cache &c, int64_t width, int
     Split s{};
     const int group = q.heads / c.heads;
     s.own_cap = cap_of(c, width, max_length);
-    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, q.type, s.own_cap, q.tokens * group, prefix.groups == 0);
+    s.own = plan_of(sequences, max_queries * group, c.heads, c.head_dim, q.type, s.own_cap, q.tokens * group, prefix.groups > 0, prefix.groups == 0);
     if (prefix.groups) {
         s.prefix_cap = cap_of(c, prefix.table_width, prefix.max_length);
-        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, q.type, s.prefix_cap, q.tokens * group, false);
-        s.slots = s.own.slots + s.prefix.slots;
+        s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, q.type, s.prefix_cap, q.tokens * group, false, false);
+        // Few own tokens, which few rows see in one go, are joined with the prefix' parts by the workgroups that have them (28 sequences
+        // with up to 300: 25.8 us, with a join of its own 32.4; 64 with up to 1024: 89.5, 86.6 with shorter chunks and a join).
+        s.joins = !s.own.wide && s.own_cap <= kJoined;
+        if (s.joins) {
+            s.own.chunk = kJoined;
+            s.own.slots = 1;
+        }
+        s.slots = s.prefix.slots + (s.joins ? 0 : s.own.slots);
     } else {
         s.slots = s.own.slots > 1 ? s.own.slots : 0;
     }
@@ -106,8 +115,9 @@ dybit_status check_sizes(const dybit_heads &q, const dybit_kv_cache &c, int64_t 
 // parts, each with every WAVES-th of them.  Bound by the latency of reading the parts, which are still in the caches: a wave asks for
 // eight of them at once.
 struct Join {
-    Phase own, prefix;
-    int32_t prefix_groups, own_slots, prefix_slots;
+    Phase own;
+    Shared shared;
+    int32_t own_slots, prefix_slots;
 };
 
 __device__ __forceinline__ void store_one(const Phase &p, int64_t at, float x)
@@ -129,19 +139,8 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : kThreads) void join_kernel
     const int i = n / heads_q, h = n - i * heads_q;
     const bool real = i < g.count;
     const int64_t row = real ? (g.first + i) * heads_q + h : 0;
-    int own = real ? (visible(p.own, g, i) + p.own.chunk - 1) / p.own.chunk : 0, before = 0;
-    if (real && p.prefix_groups) {
-        // the group that names this sequence
-        int a = 0, b = p.prefix_groups;
-        while (b - a > 1) {
-            const int mid = (a + b) >> 1;
-            if (p.prefix.members[mid] <= seq) a = mid; else b = mid;
-        }
-        if (p.prefix.members[a] <= seq && seq < p.prefix.members[a + 1]) {
-            const Segment whole = segment(p.prefix, a);
-            if (g.first >= whole.first && g.first + i < whole.first + whole.count) before = (whole.length + p.prefix.chunk - 1) / p.prefix.chunk;
-        }
-    }
+    const int own = real ? (visible(p.own, g, i) + p.own.chunk - 1) / p.own.chunk : 0;
+    const int before = real ? parts_before(p.own, p.shared, seq, g.first + i) : 0;
     // the row's slots one after the other: those of the prefix, then its own
     const int count = before + own;
     const int64_t base_slot = row * p.own.slots;
@@ -340,18 +339,20 @@ extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, 
     kv::Join j{};
     j.own = p;
     j.own.tables = tables; j.own.lengths = lengths; j.own.table_width = table_width; j.own.max_queries = max_queries; j.own.cap = s.own_cap;
-    j.own.whole = s.own.whole; j.own.causal = causal; j.own.chunk = s.own.chunk; j.own.slot0 = prefix.groups ? s.prefix.slots : 0;
+    j.own.whole = s.own.whole; j.own.causal = causal; j.own.chunk = s.own.chunk; j.own.slot0 = s.prefix.slots;
     j.own_slots = (int32_t)s.own.slots;
     if (prefix.groups) {
-        j.prefix = p;
-        j.prefix.tables = prefix.tables; j.prefix.lengths = prefix.lengths; j.prefix.members = prefix.starts;
-        j.prefix.table_width = prefix.table_width; j.prefix.max_queries = prefix.max_queries; j.prefix.cap = s.prefix_cap;
-        j.prefix.causal = 0; j.prefix.chunk = s.prefix.chunk; j.prefix.slot0 = 0;
-        j.prefix_groups = (int32_t)prefix.groups; j.prefix_slots = (int32_t)s.prefix.slots;
-        kv::launch(j.prefix, s.prefix, cache, prefix.groups, hs);
+        kv::Phase x = p;
+        x.tables = prefix.tables; x.lengths = prefix.lengths; x.members = prefix.starts;
+        x.table_width = prefix.table_width; x.max_queries = prefix.max_queries; x.cap = s.prefix_cap;
+        x.causal = 0; x.chunk = s.prefix.chunk; x.slot0 = 0;
+        j.shared = kv::Shared{prefix.lengths, prefix.starts, prefix.max_queries, s.prefix_cap, (int32_t)prefix.groups, s.prefix.chunk};
+        j.prefix_slots = (int32_t)s.prefix.slots;
+        if (s.joins) j.own.shared = j.shared;
+        kv::launch(x, s.prefix, cache, prefix.groups, hs);
     }
     kv::launch(j.own, s.own, cache, sequences, hs);
     if (s.own.whole) kv::join_left(j.own, cache.head_dim, hs);
-    else if (need) kv::join(j, cache.head_dim, max_queries, sequences, hs);
+    else if (need && !s.joins) kv::join(j, cache.head_dim, max_queries, sequences, hs);
     return launch_status();
 }
