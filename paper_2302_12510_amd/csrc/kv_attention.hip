@@ -43,7 +43,7 @@ struct Vals {
 };
 
 template <int D, int TERMS, int NT>
-__global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
+__global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;
@@ -102,9 +102,11 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 
     Rows<D, TERMS> r[NT];
     State<D> st[NT];
-    int least = 0x7fffffff;
+    int least = 0x7fffffff, parts[NT];                     // parts: that a shared prefix has left for this lane's row
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+        const int n = row0 + 16 * t + (lane & 15);
+        parts[t] = joins && n < g.count * p.group ? parts_before(p, p.shared, seg, g.first + (int)((unsigned)n / (unsigned)p.group)) : 0;
         load_rows<KB, D, TERMS>(p, g, head, row0 + 16 * t, lane, r[t]);
         st[t].clear();
         if (r[t].row >= 0) least = min(least, r[t].seen);
@@ -193,36 +195,42 @@ __global__ __launch_bounds__(kThreads, D == 256 || D * NT * TERMS >= 512 ? 1 : 2
 #pragma unroll
     for (int t = 0; t < NT; ++t) settle<VB, TERMS>(st[t], r[t].factor, ref);
     if (joins) {
-        // the prefix' parts of these rows, shared out over the waves, two at a time
+        // the prefix' parts of these rows, shared out over the waves, two at a time (256 dims: one, for the registers)
+        constexpr int AT_ONCE = D == 256 ? 1 : 2;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int heads_q = p.kv_heads * p.group;
-            const int parts = r[t].row >= 0 ? parts_before(p, p.shared, seg, r[t].row / heads_q) : 0;
-            for (int k = wave; __any(k < parts); k += 2 * kWaves) {
-                float2 stat[2];
-                float x[2][4][D / 16];
+            for (int k = wave; __any(k < parts[t]); k += AT_ONCE * kWaves) {
+                float2 stat[AT_ONCE];
+                float x[AT_ONCE][4][D / 16], m = st[t].m;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < AT_ONCE; ++b) {
                     stat[b] = float2{-__builtin_inff(), 0.0f};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int j = 0; j < D / 16; ++j) x[b][i][j] = 0.0f;
-                    if (k + b * kWaves < parts) {
+                    if (k + b * kWaves < parts[t]) {
                         const int64_t at = r[t].row * p.slots + k + b * kWaves;
                         stat[b] = *reinterpret_cast<const float2 *>(p.part_stat + 2 * at);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) heads::Pack<float, D / 16>::load(p.part_out + at * D + (D / 16) * (4 * g4 + i), x[b][i]);
                     }
+                    m = fmaxf(m, stat[b].x);
                 }
-                const float m = fmaxf(st[t].m, fmaxf(stat[0].x, stat[1].x)), base = m == -__builtin_inff() ? 0.0f : m;
-                const float a = __builtin_amdgcn_exp2f(st[t].m - base), w0 = __builtin_amdgcn_exp2f(stat[0].x - base), w1 = __builtin_amdgcn_exp2f(stat[1].x - base);
+                const float base = m == -__builtin_inff() ? 0.0f : m, keep = __builtin_amdgcn_exp2f(st[t].m - base);
                 st[t].m = m;
-                st[t].l = st[t].l * a + stat[0].y * w0 + stat[1].y * w1;
+                st[t].l *= keep;
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j)
+                for (int j = 0; j < D / 16; ++j) st[t].o[j] *= keep;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) st[t].o[j][i] = st[t].o[j][i] * a + x[0][i][j] * w0 + x[1][i][j] * w1;
+                for (int b = 0; b < AT_ONCE; ++b) {
+                    const float w = __builtin_amdgcn_exp2f(stat[b].x - base);
+                    st[t].l += stat[b].y * w;
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st[t].o[j][i] += x[b][i][j] * w;
+                }
             }
         }
     }

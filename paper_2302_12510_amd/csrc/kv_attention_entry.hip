@@ -21,6 +21,7 @@ constexpr int kThreads = 256, kWaves = 4;
 // them), they go whole, but for the last ones (Tile).
 constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
 constexpr int32_t kJoined = 512;                           // tokens behind a prefix that one workgroup joins with it
+constexpr int32_t kJoinedParts = 16;                       // and with so many parts of it: a wave takes a quarter of them, two at a time
 constexpr int32_t kShortest = 128, kLongest = 1536;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
 // fp32 is split into two halves.
@@ -80,7 +81,7 @@ Split split_of(const dybit_heads &q, const dybit_kv_cache &c, int64_t width, int
         s.prefix = plan_of(prefix.groups, prefix.max_queries * group, c.heads, c.head_dim, q.type, s.prefix_cap, q.tokens * group, false, false);
         // Few own tokens, which few rows see in one go, are joined with the prefix' parts by the workgroups that have them (28 sequences
         // with up to 300: 25.8 us, with a join of its own 32.4; 64 with up to 1024: 89.5, 86.6 with shorter chunks and a join).
-        s.joins = !s.own.wide && s.own_cap <= kJoined;
+        s.joins = !s.own.wide && s.own_cap <= kJoined && s.prefix.slots <= kJoinedParts;
         if (s.joins) {
             s.own.chunk = kJoined;
             s.own.slots = 1;

@@ -34,21 +34,20 @@ struct Share {
     int valid;                                           // tokens of the block of 16 that count
 };
 
-template <int D, int WAVES, int BUFFERS>
+template <int D, int WAVES>
 struct Lds {
-    f16x8 k[BUFFERS][WAVES][D / 32][64];
-    f16x8 v[BUFFERS][WAVES / 2][D / 16][64];
-    float sk[BUFFERS][16 * WAVES], sv[BUFFERS][16 * WAVES];
-    float top[BUFFERS][WAVES];                           // largest scale of a block's values
-    int valid[BUFFERS][WAVES];
+    f16x8 k[2][WAVES][D / 32][64];
+    f16x8 v[2][WAVES / 2][D / 16][64];
+    float sk[2][16 * WAVES], sv[2][16 * WAVES];
+    float top[2][WAVES];                           // largest scale of a block's values
+    int valid[2][WAVES];
 };
 
 template <int D, int TERMS>
 __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4) void attention_wide_kernel(const Phase p)
 {
     constexpr int WAVES = wide_waves(D, TERMS), STEP = 16 * WAVES;
-    constexpr int BUFFERS = D == 256 ? 1 : 2;            // 64 KB a step of 256 dims
-    __shared__ Lds<D, WAVES, BUFFERS> lds;
+    __shared__ Lds<D, WAVES> lds;                          // two buffers of 64 KB, or 32 for 64 dims
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     constexpr int ROWS = 16 * NT * WAVES;
     int seg, head, row0, slot = 0;
@@ -213,19 +212,18 @@ __global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4
             }
     };
     auto prepare = [&](int step) {                       // codes of `step` are in registers
-        if (step < steps) decode(share, step & (BUFFERS - 1));
+        if (step < steps) decode(share, step & 1);
         if (step + 1 < steps) fetch(share, step + 1);
     };
     prepare(0);
     __syncthreads();
     for (int step = 0; step < steps; ++step) {
-        const int buffer = step & (BUFFERS - 1), token = lo + step * STEP;
+        const int buffer = step & 1, token = lo + step * STEP;
         if (works) {
 #pragma unroll 1
             for (int sub = 0; sub < STEP / kSub; ++sub)
                 if (token + sub * kSub < hi) go(token + sub * kSub, buffer, sub);
         }
-        if (BUFFERS == 1) __syncthreads();
         prepare(step + 1);
         __syncthreads();
     }
