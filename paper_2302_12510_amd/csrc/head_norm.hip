@@ -9,6 +9,8 @@
 // Both are bound by memory: a head is read and written once (backward: read twice, written once).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "heads.h"
 
 namespace dybit {
@@ -246,17 +248,26 @@ __global__ __launch_bounds__(kSumThreads) void head_norm_sum_kernel(const float 
     else if (dwk) dwk[column - D] = x;
 }
 
-int blocks_of(int64_t tokens) { return (int)(tokens < kMostBlocks * 2 ? (tokens + 1) / 2 : kMostBlocks); }
+// Waves of a token backward: two keep kMostBlocks' waves in work from 2048 tokens on; fewer tokens are shared out more finely, down to one
+// head a wave and turn.
+int64_t backward_parts(int64_t tokens, int64_t turns)
+{
+    const int64_t wanted = std::max<int64_t>(2, kMostBlocks * kWaves / std::max<int64_t>(1, tokens));
+    return std::max<int64_t>(1, std::min(turns, wanted));
+}
+int blocks_of(int64_t tokens, int64_t parts) { return (int)std::min<int64_t>(kMostBlocks, (tokens * parts + kWaves - 1) / kWaves); }
 
 template <class T, bool BACK>
-void launch(Args &p, int V, int blocks, hipStream_t st)
+int launch(Args &p, int V, hipStream_t st)
 {
+    int blocks;
     int lanes = 1;
     while (lanes < 64 && lanes * V < p.D / 2) lanes *= 2;
     p.lanes = lanes;
     const int groups = 64 / lanes, turns = (p.heads[0] + groups - 1) / groups;
     if (BACK) {
-        p.parts = turns < 2 ? turns : 2;          // two tokens a block
+        p.parts = (int)backward_parts(p.tokens, turns);
+        blocks = blocks_of(p.tokens, p.parts);
     } else {
         p.parts = p.tokens >= 4096 ? 1 : turns;
         blocks = (int)((p.tokens * p.parts + kWaves - 1) / kWaves);
@@ -265,11 +276,12 @@ void launch(Args &p, int V, int blocks, hipStream_t st)
     const dim3 grid((unsigned)blocks), block(kThreads);
 #define DYBIT_HN(V, K) hipLaunchKernelGGL((head_norm_kernel<T, V, K, BACK>), grid, block, 0, st, p)
     if constexpr (sizeof(T) == 2 && !BACK)
-        if (V == 8) { DYBIT_HN(8, 1); return; }
+        if (V == 8) { DYBIT_HN(8, 1); return blocks; }
     if (V == 4) DYBIT_HN(4, 1);
     else if (V == 2) DYBIT_HN(2, 1);
     else DYBIT_HN(1, 4);
 #undef DYBIT_HN
+    return blocks;
 }
 
 bool aligned_floats(const float *p, int n) { return reinterpret_cast<uintptr_t>(p) % (4u * (unsigned)n) == 0; }
@@ -315,12 +327,12 @@ dybit_status run(bool back, const dybit_heads *g, const dybit_heads *x, const dy
     p.D = D; p.half = rotary / 2; p.neighbours = neighbours; p.eps = eps; p.partial = workspace;
     p.err = async_error_word();
     if (!p.err) return DYBIT_ERR_HIP;
-    const int blocks = back ? blocks_of(p.tokens) : 0;
+    int blocks = 0;
     if (p.tokens) {
         switch (x[0].type) {
-            case DYBIT_F32: back ? launch<float, true>(p, V, blocks, st) : launch<float, false>(p, V, blocks, st); break;
-            case DYBIT_F16: back ? launch<_Float16, true>(p, V, blocks, st) : launch<_Float16, false>(p, V, blocks, st); break;
-            default: back ? launch<__bf16, true>(p, V, blocks, st) : launch<__bf16, false>(p, V, blocks, st); break;
+            case DYBIT_F32: blocks = back ? launch<float, true>(p, V, st) : launch<float, false>(p, V, st); break;
+            case DYBIT_F16: blocks = back ? launch<_Float16, true>(p, V, st) : launch<_Float16, false>(p, V, st); break;
+            default: blocks = back ? launch<__bf16, true>(p, V, st) : launch<__bf16, false>(p, V, st); break;
         }
     }
     if (back)
@@ -344,7 +356,9 @@ extern "C" dybit_status dybit_head_norm_rope(dybit_heads q, dybit_heads k, const
 extern "C" size_t dybit_head_norm_rope_bwd_workspace(int64_t tokens, int32_t heads, int32_t head_dim)
 {
     if (tokens < 0 || heads < 0 || head_dim < 1) return 0;
-    return (size_t)(tokens ? dybit::headnorm::blocks_of(tokens) : 1) * 2 * (size_t)head_dim;
+    // turns at the heads depend on the alignment of the call's tensors: at most one a head
+    const int64_t parts = dybit::headnorm::backward_parts(tokens, heads);
+    return (size_t)(tokens ? dybit::headnorm::blocks_of(tokens, parts) : 1) * 2 * (size_t)head_dim;
 }
 
 extern "C" dybit_status dybit_head_norm_rope_bwd(dybit_heads grad_q, dybit_heads grad_k, dybit_heads q, dybit_heads k,
