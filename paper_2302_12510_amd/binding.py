@@ -116,11 +116,15 @@ class _Ctypes:
         return lib().dybit_head_norm_rope(_heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _typed(positions, torch.int64), _ptr(cos), _ptr(sin),
                                           cos.shape[0], 2 * cos.shape[1], bool(neighbours), eps, _heads(q_out), _heads(k_out), _stream(stream)), q_out, k_out
 
-    def dybit_head_norm_rope_bwd(self, gq, gk, q, k, q_weight, k_weight, positions, cos, sin, rows, rotary, neighbours, eps, dq, dk, dwq, dwk, work,
-                                 stream):
-        return lib().dybit_head_norm_rope_bwd(_heads(gq), _heads(gk), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _typed(positions, torch.int64),
-                                              _ptr(cos), _ptr(sin), rows, rotary, neighbours, eps, _heads(dq), _heads(dk), _ptr(dwq), _ptr(dwk),
-                                              _ptr(work), _stream(stream))
+    def head_norm_rope_bwd(self, grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours, out):
+        _check_rotation(q, q_weight, k, k_weight, positions, cos, sin)
+        dq, dk = out if out is not None else (self.empty_rows(q), None if k is None else self.empty_rows(k))
+        D, heads = q.shape[2], q.shape[1] + (0 if k is None else k.shape[1])
+        dwq, dwk = self.empty(q, True, D), None if k is None else self.empty(q, True, D)
+        work = self.empty(q, True, int(lib().dybit_head_norm_rope_bwd_workspace(q.shape[0], heads, D)))
+        return lib().dybit_head_norm_rope_bwd(_heads(grad_q), _heads(grad_k), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight),
+                                              _typed(positions, torch.int64), _ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], bool(neighbours),
+                                              eps, _heads(dq), _heads(dk), _ptr(dwq), _ptr(dwk), _ptr(work), _stream()), dq, dk, dwq, dwk
 
     def dybit_kv_append(self, keys, values, slots, cache, stream):
         return lib().dybit_kv_append(_heads(keys), _heads(values), _typed(slots, torch.int64), _kv_cache(cache), _stream(stream))
@@ -757,14 +761,9 @@ def dybit_head_norm_rope_bwd(grad_q: torch.Tensor, grad_k: torch.Tensor | None, 
     if stream is not None:                                   # the workspace has to be that stream's
         with torch.cuda.stream(stream):
             return dybit_head_norm_rope_bwd(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours, out)
-    _check_rotation(q, q_weight, k, k_weight, positions, cos, sin)
-    dq, dk = out if out is not None else (_n().empty_rows(q), None if k is None else _n().empty_rows(k))
-    D, heads = q.shape[2], q.shape[1] + (0 if k is None else k.shape[1])
-    dwq, dwk = _n().empty(q, True, D), None if k is None else _n().empty(q, True, D)
-    work = _n().empty(q, True, int(lib().dybit_head_norm_rope_bwd_workspace(q.shape[0], heads, D)))
-    _check(_n().dybit_head_norm_rope_bwd(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, cos.shape[0], 2 * cos.shape[1],
-                                         bool(neighbours), eps, dq, dk, dwq, dwk, work, None), "dybit_head_norm_rope_bwd")
-    return dq, dk, dwq, dwk
+    status, *grads = _n().head_norm_rope_bwd(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours, out)
+    _check(status, "dybit_head_norm_rope_bwd")
+    return tuple(grads)
 
 
 def dybit_kv_append(keys: torch.Tensor, values: torch.Tensor, slots: torch.Tensor, cache: KVCache, stream=None) -> None:

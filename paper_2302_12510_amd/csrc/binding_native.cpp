@@ -323,6 +323,54 @@ PyObject *kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// Arguments that the head norms' passes share, checked: queries and keys, their weights, positions, tables, eps, neighbours.
+struct HeadNorm {
+    dybit_heads x[2];
+    const float *w[2];
+    const int64_t *positions;
+    const float *cos, *sin;
+    int64_t rows;
+    int32_t rotary, neighbours;
+    float eps;
+    explicit HeadNorm(PyObject *const *args)               // q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours
+    {
+        for (int a = 0; a < 2; ++a) {
+            x[a] = head_rows(args[a]);
+            w[a] = (const float *)typed_address(args[2 + a], at::kFloat, "float32");
+        }
+        positions = argument<const int64_t *>(args[4]);
+        cos = (const float *)typed_address(args[5], at::kFloat, "float32");
+        sin = (const float *)typed_address(args[6], at::kFloat, "float32");
+        bool fits = args[0] != Py_None && THPVariable_Check(args[4]) && THPVariable_Check(args[5]) && THPVariable_Check(args[6]);
+        for (int a = 0; fits && a < 2; ++a)
+            fits = args[a] == Py_None || (THPVariable_Check(args[2 + a]) && THPVariable_Unpack(args[2 + a]).numel() == x[a].head_dim);
+        if (fits) {
+            const at::Tensor &p = THPVariable_Unpack(args[4]), &c = THPVariable_Unpack(args[5]);
+            fits = p.dim() == 1 && p.size(0) == x[0].tokens && c.dim() == 2 && c.sizes() == THPVariable_Unpack(args[6]).sizes();
+        }
+        if (!fits) { PyErr_SetString(PyExc_ValueError, "expected tables [positions][pairs], a position a token and a weight an element of a head"); throw PythonError(); }
+        const at::Tensor &c = THPVariable_Unpack(args[5]);
+        rows = c.size(0);
+        rotary = (int32_t)(2 * c.size(1));
+        eps = real(args[7]);
+        neighbours = truth(args[8]);
+    }
+};
+
+// New references to the outputs: those of the pair `given`, or (None) tensors like `like`.
+void outputs_like(PyObject *given, PyObject *const *like, PyObject **outs)
+{
+    if (given != Py_None && (!PyTuple_Check(given) || PyTuple_GET_SIZE(given) != 2)) { PyErr_SetString(PyExc_TypeError, "expected a pair of outputs"); throw PythonError(); }
+    for (int a = 0; a < 2; ++a) {
+        if (given != Py_None) Py_INCREF(outs[a] = PyTuple_GET_ITEM(given, a));
+        else if (like[a] == Py_None) Py_INCREF(outs[a] = Py_None);
+        else {
+            const at::Tensor &t = THPVariable_Unpack(like[a]);
+            outs[a] = THPVariable_Wrap(at::empty(t.sizes(), t.options()));
+        }
+    }
+}
+
 // dybit_head_norm_rope with its checks of shapes and its outputs: (q, k, q_weight, k_weight, positions, cos, sin, eps, neighbours,
 // (q_out, k_out) or None, stream) -> (status, q_out, k_out).  Two outputs and the checks from Python were 1.5 us of a call's 6.7.
 PyObject *head_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -334,41 +382,53 @@ PyObject *head_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     PyObject *outs[2] = {nullptr, nullptr};
     try {
-        const dybit_heads x[2] = {head_rows(args[0]), head_rows(args[1])};
-        const float *w[2] = {(const float *)typed_address(args[2], at::kFloat, "float32"), (const float *)typed_address(args[3], at::kFloat, "float32")};
-        const int64_t *positions = argument<const int64_t *>(args[4]);
-        const float *cos = (const float *)typed_address(args[5], at::kFloat, "float32"), *sin = (const float *)typed_address(args[6], at::kFloat, "float32");
-        bool fits = args[0] != Py_None && THPVariable_Check(args[4]) && THPVariable_Check(args[5]) && THPVariable_Check(args[6]);
-        for (int a = 0; fits && a < 2; ++a)
-            fits = args[a] == Py_None || (THPVariable_Check(args[2 + a]) && THPVariable_Unpack(args[2 + a]).numel() == x[a].head_dim);
-        if (fits) {
-            const at::Tensor &p = THPVariable_Unpack(args[4]), &c = THPVariable_Unpack(args[5]);
-            fits = p.dim() == 1 && p.size(0) == x[0].tokens && c.dim() == 2 && c.sizes() == THPVariable_Unpack(args[6]).sizes();
-        }
-        if (!fits) { PyErr_SetString(PyExc_ValueError, "expected tables [positions][pairs], a position a token and a weight an element of a head"); throw PythonError(); }
-        const at::Tensor &c = THPVariable_Unpack(args[5]);
-        const float eps = real(args[7]);
-        const int32_t neighbours = truth(args[8]);
+        const HeadNorm h(args);
         const dybit_stream stream = stream_of(args[10]);
-        if (args[9] != Py_None) {
-            if (!PyTuple_Check(args[9]) || PyTuple_GET_SIZE(args[9]) != 2) { PyErr_SetString(PyExc_TypeError, "expected (q_out, k_out)"); throw PythonError(); }
-            for (int a = 0; a < 2; ++a) Py_INCREF(outs[a] = PyTuple_GET_ITEM(args[9], a));
-        } else {
-            for (int a = 0; a < 2; ++a) {
-                if (args[a] == Py_None) {
-                    Py_INCREF(outs[a] = Py_None);
-                } else {
-                    const at::Tensor &t = THPVariable_Unpack(args[a]);
-                    outs[a] = THPVariable_Wrap(at::empty(t.sizes(), t.options()));
-                }
-            }
-        }
+        outputs_like(args[9], args, outs);
         const dybit_heads y[2] = {head_rows(outs[0]), head_rows(outs[1])};
         dybit_status st;
         Py_BEGIN_ALLOW_THREADS
-        st = dybit_head_norm_rope(x[0], x[1], w[0], w[1], positions, cos, sin, c.size(0), (int32_t)(2 * c.size(1)), neighbours, eps, y[0], y[1], stream);
+        st = dybit_head_norm_rope(h.x[0], h.x[1], h.w[0], h.w[1], h.positions, h.cos, h.sin, h.rows, h.rotary, h.neighbours, h.eps, y[0], y[1], stream);
         Py_END_ALLOW_THREADS
         return Py_BuildValue("iNN", (int)st, outs[0], outs[1]);
+    } catch (const PythonError &) {
+        Py_XDECREF(outs[0]);
+        Py_XDECREF(outs[1]);
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// dybit_head_norm_rope_bwd on the current stream, with its checks, outputs and workspace: (grad_q, grad_k, then as above up to neighbours,
+// (dq, dk) or None) -> (status, dq, dk, q_weight_grad, k_weight_grad).
+PyObject *head_norm_rope_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 12) {
+        PyErr_Format(PyExc_TypeError, "expected 12 arguments, got %zd", n);
+        return nullptr;
+    }
+    PyObject *outs[2] = {nullptr, nullptr};
+    try {
+        const dybit_heads g[2] = {head_rows(args[0]), head_rows(args[1])};
+        const HeadNorm h(args + 2);
+        outputs_like(args[11], args + 2, outs);
+        const dybit_heads y[2] = {head_rows(outs[0]), head_rows(outs[1])};
+        const int64_t D = h.x[0].head_dim;
+        const bool keys = args[3] != Py_None;
+        const auto options = THPVariable_Unpack(args[2]).options().dtype(at::kFloat);
+        const at::Tensor dwq = at::empty({D}, options), dwk = keys ? at::empty({D}, options) : at::Tensor();
+        const size_t need = 4 * dybit_head_norm_rope_bwd_workspace(h.x[0].tokens, h.x[0].heads + h.x[1].heads, (int32_t)D);
+        const c10::DataPtr work = need ? c10::GetAllocator(c10::DeviceType::CUDA)->allocate(need) : c10::DataPtr();
+        dybit_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = dybit_head_norm_rope_bwd(g[0], g[1], h.x[0], h.x[1], h.w[0], h.w[1], h.positions, h.cos, h.sin, h.rows, h.rotary, h.neighbours, h.eps, y[0], y[1],
+                                      (float *)dwq.data_ptr(), keys ? (float *)dwk.data_ptr() : nullptr, (float *)work.get(),
+                                      (dybit_stream)c10::hip::getCurrentHIPStream().stream());
+        Py_END_ALLOW_THREADS
+        PyObject *wk = keys ? THPVariable_Wrap(dwk) : Py_None;
+        if (!keys) Py_INCREF(wk);
+        return Py_BuildValue("iNNNN", (int)st, outs[0], outs[1], THPVariable_Wrap(dwq), wk);
     } catch (const PythonError &) {
         Py_XDECREF(outs[0]);
         Py_XDECREF(outs[1]);
@@ -425,7 +485,8 @@ PyMethodDef methods[] = {
     {"dybit_gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr}, DYBIT_ENTRY(dybit_gemm_ex), DYBIT_ENTRY(dybit_gemm_wb), DYBIT_ENTRY(dybit_gemm_wb_rc), DYBIT_ENTRY(dybit_gemm_pc),
     DYBIT_ENTRY(dybit_conv2d), DYBIT_ENTRY(dybit_conv2d_ex), DYBIT_ENTRY(dybit_conv2d_wb), DYBIT_ENTRY(dybit_conv2d_wb_rc), DYBIT_ENTRY(dybit_conv2d_pc),
     DYBIT_ENTRY(dybit_dwconv2d), DYBIT_ENTRY(dybit_dwconv2d_wb), DYBIT_ENTRY(dybit_group_conv2d), DYBIT_ENTRY(dybit_maxpool2d_codes),
-    {"head_norm_rope", (PyCFunction)(void (*)(void))head_norm_rope, METH_FASTCALL, nullptr}, DYBIT_ENTRY(dybit_head_norm_rope_bwd), DYBIT_ENTRY(dybit_kv_append), DYBIT_ENTRY(dybit_kv_copy_pages),
+    {"head_norm_rope", (PyCFunction)(void (*)(void))head_norm_rope, METH_FASTCALL, nullptr},
+    {"head_norm_rope_bwd", (PyCFunction)(void (*)(void))head_norm_rope_bwd, METH_FASTCALL, nullptr}, DYBIT_ENTRY(dybit_kv_append), DYBIT_ENTRY(dybit_kv_copy_pages),
     {"dybit_kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
     {"empty_rows", (PyCFunction)empty_rows, METH_O, nullptr},
     {"dybit_packed_bytes", (PyCFunction)(void (*)(void))packed_bytes, METH_FASTCALL, nullptr},
