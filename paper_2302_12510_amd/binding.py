@@ -126,13 +126,13 @@ class _Ctypes:
                                               _typed(positions, torch.int64), _ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], bool(neighbours),
                                               eps, _heads(dq), _heads(dk), _ptr(dwq), _ptr(dwk), _ptr(work), _stream()), dq, dk, dwq, dwk
 
-    def dybit_kv_append(self, keys, values, slots, cache, stream):
+    def kv_append(self, keys, values, slots, cache, stream):
         return lib().dybit_kv_append(_heads(keys), _heads(values), _typed(slots, torch.int64), _kv_cache(cache), _stream(stream))
 
-    def dybit_kv_copy_pages(self, cache, src, dst, n, stream):
+    def kv_copy_pages(self, cache, src, dst, n, stream):
         return lib().dybit_kv_copy_pages(_kv_cache(cache), _typed(src, torch.int32), _typed(dst, torch.int32), n, _stream(stream))
 
-    def dybit_kv_attention(self, q, cache, tables, width, lengths, starts, sequences, max_queries, max_length, causal, scale, prefix, out):
+    def kv_attention(self, q, cache, tables, width, lengths, starts, sequences, max_queries, max_length, causal, scale, prefix, out):
         x, c, h = _kv_prefix(prefix), _kv_cache(cache), _heads(q)
         need = int(lib().dybit_kv_attention_workspace_bytes(h, c, width, sequences, max_queries, max_length, x))
         work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
@@ -771,7 +771,7 @@ def dybit_kv_append(keys: torch.Tensor, values: torch.Tensor, slots: torch.Tenso
     skipped) of one layer's cache."""
     if slots.numel() != keys.shape[0]:
         raise ValueError("expected a slot for every token")
-    _check(_n().dybit_kv_append(keys, values, slots, cache, stream), "dybit_kv_append")
+    _check(_n().kv_append(keys, values, slots, cache, stream), "dybit_kv_append")
 
 
 def dybit_kv_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
@@ -779,7 +779,7 @@ def dybit_kv_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, st
     n = src.numel()
     if dst.numel() != n:
         raise ValueError("expected as many pages to copy to as to copy from")
-    _check(_n().dybit_kv_copy_pages(cache, src, dst, n, stream), "dybit_kv_copy_pages")
+    _check(_n().kv_copy_pages(cache, src, dst, n, stream), "dybit_kv_copy_pages")
 
 
 def dybit_kv_attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor | None = None,
@@ -799,6 +799,6 @@ def dybit_kv_attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, le
         out = _n().empty_rows(q)
     if scale is None:
         scale = q.shape[2] ** -0.5
-    _check(_n().dybit_kv_attention(q, cache, tables, tables.shape[1], lengths, starts, n, max_queries, max_length, causal, scale, prefix, out),
+    _check(_n().kv_attention(q, cache, tables, tables.shape[1], lengths, starts, n, max_queries, max_length, causal, scale, prefix, out),
            "dybit_kv_attention")
     return out

@@ -476,7 +476,8 @@ PyObject *packed_bytes(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
 }
 
-#define DYBIT_ENTRY(name) {#name, (PyCFunction)(void (*)(void))Entry<&name>::call, METH_FASTCALL, nullptr}
+#define DYBIT_NAMED(python, name) {python, (PyCFunction)(void (*)(void))Entry<&name>::call, METH_FASTCALL, nullptr}
+#define DYBIT_ENTRY(name) DYBIT_NAMED(#name, name)
 PyMethodDef methods[] = {
     DYBIT_ENTRY(dybit_absmax_scale), DYBIT_ENTRY(dybit_absmax_scale_ws), DYBIT_ENTRY(dybit_scale_from_absmax),
     DYBIT_ENTRY(dybit_quantize), DYBIT_ENTRY(dybit_quantize_absmax), DYBIT_ENTRY(dybit_quantize_pad),
@@ -486,8 +487,8 @@ PyMethodDef methods[] = {
     DYBIT_ENTRY(dybit_conv2d), DYBIT_ENTRY(dybit_conv2d_ex), DYBIT_ENTRY(dybit_conv2d_wb), DYBIT_ENTRY(dybit_conv2d_wb_rc), DYBIT_ENTRY(dybit_conv2d_pc),
     DYBIT_ENTRY(dybit_dwconv2d), DYBIT_ENTRY(dybit_dwconv2d_wb), DYBIT_ENTRY(dybit_group_conv2d), DYBIT_ENTRY(dybit_maxpool2d_codes),
     {"head_norm_rope", (PyCFunction)(void (*)(void))head_norm_rope, METH_FASTCALL, nullptr},
-    {"head_norm_rope_bwd", (PyCFunction)(void (*)(void))head_norm_rope_bwd, METH_FASTCALL, nullptr}, DYBIT_ENTRY(dybit_kv_append), DYBIT_ENTRY(dybit_kv_copy_pages),
-    {"dybit_kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
+    {"head_norm_rope_bwd", (PyCFunction)(void (*)(void))head_norm_rope_bwd, METH_FASTCALL, nullptr}, DYBIT_NAMED("kv_append", dybit_kv_append), DYBIT_NAMED("kv_copy_pages", dybit_kv_copy_pages),
+    {"kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
     {"empty_rows", (PyCFunction)empty_rows, METH_O, nullptr},
     {"dybit_packed_bytes", (PyCFunction)(void (*)(void))packed_bytes, METH_FASTCALL, nullptr},
     {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, nullptr},

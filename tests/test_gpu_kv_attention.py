@@ -76,6 +76,30 @@ def test_many_sequences_share_a_prefix():
     check_attention(rng, world, None, 8, "fp32", sizes=[50])
 
 
+@pytest.mark.parametrize("D,dtype", [(64, "fp32"), (128, "bf16"), (256, "fp16"), (256, "fp32")])
+@pytest.mark.parametrize("own,prefix", [([5, 0, 300], [128]), ([5, 0, 300], [2900]), ([700, 0, 520], [1300]), ([513, 1, 2], [0])])
+@pytest.mark.parametrize("new", [None, [2, 5, 0], [40, 1, 0]])
+def test_prefixes_of_few_and_of_many_parts(D, dtype, own, prefix, new):
+    """Own tokens that are joined with the prefix in place, and those that a pass of its own joins; queries in front of the own tokens."""
+    rng = np.random.default_rng(len(own) + own[0] + prefix[0] + D)
+    check_attention(rng, World(rng, own, 2, D, (4, 8), 32, prefixes=prefix), new, 6, dtype, sizes=[3])
+
+
+def test_prefix_of_a_group_with_more_queries_than_said():
+    """Queries past max_queries get no prefix, and the flag says so; the others are as they were."""
+    rng = np.random.default_rng(13)
+    world = World(rng, [20, 30, 40], 1, 64, (8, 8), 16, prefixes=[100])
+    q, _ = typed(rng.standard_normal((3, 2, 64)), "fp32")
+    args = (q, world.cache(), i32(world.tables), i32(world.lengths))
+    prefix = lambda n: B.SharedPrefix(i32(world.prefix_tables), i32(world.prefix_lengths), i32([0, 3]), n)  # noqa: E731
+    want, alone = B.dybit_kv_attention(*args, prefix=prefix(3)), B.dybit_kv_attention(*args)
+    assert B.dybit_get_last_async_error() == B.OK
+    got = B.dybit_kv_attention(*args, prefix=prefix(2))
+    assert B.dybit_get_last_async_error() == B.ERR_INVALID_ARG
+    assert torch.equal(got[:2], want[:2])
+    torch.testing.assert_close(got[2], alone[2], rtol=1e-5, atol=1e-6)
+
+
 def test_groups_that_leave_sequences_out():
     rng = np.random.default_rng(6)
     world = World(rng, [10, 20, 30, 40], 1, 64, (8, 8), 16, prefixes=[100])

@@ -99,3 +99,9 @@ def test_attention_workspace():
     assert attention(c=cache(pages=1 << 20), width=4096, size=long - 1) == B.ERR_INVALID_ARG
     assert attention(c=cache(pages=1 << 20), width=4096, work=None) == B.ERR_NULL
     assert attention(c=cache(pages=1 << 20), width=4096, work=ODD) == B.ERR_ALIGNMENT
+
+
+@pytest.mark.parametrize("name", ["head_norm_rope", "head_norm_rope_bwd", "kv_append", "kv_copy_pages", "kv_attention"])
+def test_native_calls_check_their_argument_count(name):
+    with pytest.raises(TypeError, match="arguments"):
+        getattr(B._n(), name)()
