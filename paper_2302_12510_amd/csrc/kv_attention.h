@@ -5,6 +5,7 @@
 namespace dybit {
 namespace kv {
 
+constexpr int kCus = 256;                              // compute units
 struct Left;
 
 // A shared prefix as those see it that join its parts with a sequence's own tokens.
@@ -103,7 +104,7 @@ __device__ __forceinline__ int visible(const Phase &p, const Segment &g, int i)
 // last turn is a short one too.  Which
 // they are depends on the segments' numbers of queries, so workgroups find their tile themselves and leave word of it for the join.
 // Parts lie at [left-over tile][kMostParts][row of the tile].
-constexpr int kCus = 256, kMostParts = 8;
+constexpr int kMostParts = 8;
 struct Left { int seg, head, tile, parts; };           // a left-over tile, for the join; the last one of kCus: how many there are (seg)
 struct Tile {
     int seg, head, tile;
@@ -174,6 +175,7 @@ struct Plan {
     bool wide;                                         // kv_attention_wide.hip, else kv_attention.hip
     int32_t tiles16;                                   // 16-row tiles of a wave of the latter: 1 or 2
     bool whole;                                        // Phase::whole
+    int32_t waves;                                     // of a workgroup of the wide kernel
     int32_t chunk;
     int64_t row_tiles, slots, tiles;                   // tiles: at most so many, of all segments and key heads
 };
@@ -186,9 +188,15 @@ void launch_wide_k8v8(const Phase &p, const Plan &plan, int D, int terms, int64_
 void launch_wide_k8v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
 void launch_wide_k4v8(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
 void launch_wide_k4v4(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st);
-// The wide kernel: rows of a wave, and waves of a workgroup.  Eight waves leave a wave 256 registers; four, 512.
+// The wide kernel: rows of a wave, and waves of a workgroup: eight, or four where a wave needs more than the 256 registers that eight
+// leave it, and where four hold the rows of any segment and there are segments enough to fill the device (64 sequences of 2048 tokens,
+// 8 key heads of 128 dims, 96 rows: eight 135 us, four 107; one sequence of 8192: 29 and 37, with twice the parts).
 constexpr int kWideRows = 32;
-constexpr int wide_waves(int D, int terms) { return D * terms >= 256 ? 4 : 8; }
+constexpr bool wide_registers(int D, int terms) { return D * terms >= 256; }
+constexpr int wide_waves(int D, int terms, int64_t most_rows, int64_t columns)
+{
+    return wide_registers(D, terms) || (most_rows <= 4 * kWideRows && columns >= kCus) ? 4 : 8;
+}
 
 }  // namespace kv
 }  // namespace dybit

@@ -13,12 +13,15 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 
 // ---- the plan ---------------------------------------------------------------------------------------------------------------------
-// Up to 32 rows of a segment are one or two tiles of a wave, whose waves share the keys of a chunk out; more go to the wide kernel,
-// whose waves share the rows out.  The tokens of a segment go to workgroups in chunks: as many as the device holds workgroups at once
-// (kHeld, by the kernels' registers), were all segments as long as the longest, since fewer leave it idle and more add their start and their
-// partial results (4 (D + 2) bytes a row, written and read back); but no longer ones than kLongest for few rows, which keeps batches of
-// very different lengths even; twice as many behind a prefix, where there is a join anyway.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be joined with
-// them), they go whole, but for the last ones (Tile).
+// Up to kFew rows of a segment are tiles of 16 or 32 of a wave, whose waves share the keys of a chunk out; more go to the wide kernel,
+// whose waves share the rows out (64 sequences of 2048 tokens, 128 dims, 8 bits, us: 36 rows 100 as tiles, 132 wide; 64 rows 140, 134;
+// 96 rows 185, 135; 16 sequences, 256 dims: 64 rows 81, 104; 128 rows 141, 120).
+// The tokens of a segment go to workgroups in chunks: as many as the device holds workgroups at once (kHeld, by the kernels' registers;
+// kHeldWide waves), were all segments as long as the longest, since fewer leave it idle and more add their start and their partial
+// results (4 (D + 2) bytes a row, written and read back); twice as many behind a prefix, where there is a join anyway; but no longer ones
+// than kLongest for few rows, which keeps batches of very different lengths even.  Where tiles of the wide kernel alone are more
+// than the device holds (and nothing else is to be joined with them), they go whole, but for the last ones (Tile).
+constexpr int64_t kFew = 64;
 constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
 constexpr int32_t kJoined = 512;                           // tokens behind a prefix that one workgroup joins with it
 constexpr int32_t kJoinedParts = 16;                       // and with so many parts of it: a wave takes a quarter of them, two at a time
@@ -30,9 +33,9 @@ int terms_of(int type) { return type == DYBIT_F32 ? 2 : 1; }
 Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, int64_t cap, int64_t all_rows, bool behind, bool may_be_whole)
 {
     Plan p{};
-    p.wide = max_rows > 32;
+    p.wide = max_rows > kFew;
     p.tiles16 = max_rows > 16 && D < 256 ? 2 : 1;         // two tiles of 256 dims do not fit the registers
-    const int waves = wide_waves(D, terms_of(type));
+    const int waves = p.waves = wide_waves(D, terms_of(type), max_rows, segments * kv_heads);
     const int64_t rows = p.wide ? kWideRows * waves : 16 * p.tiles16;
     p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
     const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
@@ -53,7 +56,7 @@ struct Split {
     // parts of rows in the workspace
     size_t parts(const dybit_heads &q) const
     {
-        if (own.whole) return (size_t)(kCus - 1) * kMostParts * (size_t)(kWideRows * wide_waves(q.head_dim, terms_of(q.type)));
+        if (own.whole) return (size_t)(kCus - 1) * kMostParts * (size_t)(kWideRows * own.waves);
         return (size_t)slots * (size_t)q.tokens * (size_t)q.heads;
     }
     size_t bytes(const dybit_heads &q) const { return parts(q) * (size_t)(q.head_dim + 2) * 4 + (own.whole ? (size_t)kLeftBytes : 0); }
@@ -266,9 +269,9 @@ __global__ __launch_bounds__(kThreads) void join_left_kernel(const Phase p, int 
     }
 }
 
-void join_left(const Phase &p, int D, hipStream_t st)
+void join_left(const Phase &p, const Plan &plan, int D, hipStream_t st)
 {
-    const int rows = kWideRows * wide_waves(D, terms_of(p.type));
+    const int rows = kWideRows * plan.waves;
     const dim3 grid((unsigned)((kCus - 1) * (rows / 16))), block(kThreads);
     if (D == 64) hipLaunchKernelGGL(join_left_kernel<64>, grid, block, 0, st, p, rows);
     else if (D == 128) hipLaunchKernelGGL(join_left_kernel<128>, grid, block, 0, st, p, rows);
@@ -353,7 +356,7 @@ extern "C" dybit_status dybit_kv_attention(dybit_heads q, dybit_kv_cache cache, 
         kv::launch(x, s.prefix, cache, prefix.groups, hs);
     }
     kv::launch(j.own, s.own, cache, sequences, hs);
-    if (s.own.whole) kv::join_left(j.own, cache.head_dim, hs);
+    if (s.own.whole) kv::join_left(j.own, s.own, cache.head_dim, hs);
     else if (need && !s.joins) kv::join(j, cache.head_dim, max_queries, sequences, hs);
     return launch_status();
 }

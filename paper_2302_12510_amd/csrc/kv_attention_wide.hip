@@ -43,10 +43,10 @@ struct Lds {
     int valid[2][WAVES];
 };
 
-template <int D, int TERMS>
-__global__ __launch_bounds__(64 * wide_waves(D, TERMS), wide_waves(D, TERMS) / 4) void attention_wide_kernel(const Phase p)
+template <int D, int TERMS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void attention_wide_kernel(const Phase p)
 {
-    constexpr int WAVES = wide_waves(D, TERMS), STEP = 16 * WAVES;
+    constexpr int STEP = 16 * WAVES;
     __shared__ Lds<D, WAVES> lds;                          // two buffers of 64 KB, or 32 for 64 dims
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     constexpr int ROWS = 16 * NT * WAVES;
@@ -242,9 +242,13 @@ template <int D>
 void launch_d(const Phase &p, const Plan &plan, int terms, int64_t segments, hipStream_t st)
 {
     const dim3 grid = plan.whole ? dim3((unsigned)(plan.tiles + kCus)) : dim3((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots);
-    const dim3 block((unsigned)(64 * wide_waves(D, terms)));
-    if (terms == 1) hipLaunchKernelGGL((attention_wide_kernel<D, 1>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((attention_wide_kernel<D, 2>), grid, block, 0, st, p);
+    const dim3 block((unsigned)(64 * plan.waves));
+    if constexpr (!wide_registers(D, 1))
+        if (plan.waves == 8 && terms == 1) { hipLaunchKernelGGL((attention_wide_kernel<D, 1, 8>), grid, block, 0, st, p); return; }
+    if constexpr (!wide_registers(D, 2))
+        if (plan.waves == 8) { hipLaunchKernelGGL((attention_wide_kernel<D, 2, 8>), grid, block, 0, st, p); return; }
+    if (terms == 1) hipLaunchKernelGGL((attention_wide_kernel<D, 1, 4>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((attention_wide_kernel<D, 2, 4>), grid, block, 0, st, p);
 }
 
 }  // namespace
