@@ -42,7 +42,8 @@ struct Vals {
     f32x4 scale[2];
 };
 
-template <int D, int TERMS, int NT>
+// JOINS: the rows are joined with what a shared prefix has left for them (in a kernel of its own: the others lose 2 to 7 % by it).
+template <int D, int TERMS, int NT, bool JOINS>
 __global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
@@ -57,7 +58,7 @@ __global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void atten
     last = last < g.count ? last : g.count - 1;
     const int lo = slot * p.chunk, most = visible(p, g, last);
     const int hi = most - lo < p.chunk ? most : lo + p.chunk;
-    const bool joins = p.shared.groups > 0, parted = p.part_out && !joins;
+    const bool parted = p.part_out && !JOINS;
     if (lo >= hi && parted) return;
 
     // the pages of this wave's blocks of 16 tokens, one a lane: block j is step wave + 4 (j / 2), half j % 2
@@ -105,8 +106,10 @@ __global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void atten
     int least = 0x7fffffff, parts[NT];                     // parts: that a shared prefix has left for this lane's row
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int n = row0 + 16 * t + (lane & 15);
-        parts[t] = joins && n < g.count * p.group ? parts_before(p, p.shared, seg, g.first + (int)((unsigned)n / (unsigned)p.group)) : 0;
+        if constexpr (JOINS) {
+            const int n = row0 + 16 * t + (lane & 15);
+            parts[t] = n < g.count * p.group ? parts_before(p, p.shared, seg, g.first + (int)((unsigned)n / (unsigned)p.group)) : 0;
+        }
         load_rows<KB, D, TERMS>(p, g, head, row0 + 16 * t, lane, r[t]);
         st[t].clear();
         if (r[t].row >= 0) least = min(least, r[t].seen);
@@ -194,7 +197,7 @@ __global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void atten
     __shared__ float s_m[2][NT][16], s_l[2][NT][16], s_o[2][NT][D / 4][64];
 #pragma unroll
     for (int t = 0; t < NT; ++t) settle<VB, TERMS>(st[t], r[t].factor, ref);
-    if (joins) {
+    if constexpr (JOINS) {
         // the prefix' parts of these rows, shared out over the waves, two at a time (256 dims: one, for the registers)
         constexpr int AT_ONCE = D == 256 ? 1 : 2;
 #pragma unroll
@@ -274,8 +277,13 @@ template <int D, int TERMS>
 void launch_d(const Phase &p, const Plan &plan, int64_t segments, hipStream_t st)
 {
     const dim3 grid((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots), block(kThreads);
-    if (D == 256 || plan.tiles16 == 1) hipLaunchKernelGGL((attention_kernel<D, TERMS, 1>), grid, block, 0, st, p);
-    else if constexpr (D < 256) hipLaunchKernelGGL((attention_kernel<D, TERMS, 2>), grid, block, 0, st, p);
+    const bool joins = p.shared.groups > 0;
+#define DYBIT_KV(NT) if (joins) hipLaunchKernelGGL((attention_kernel<D, TERMS, NT, true>), grid, block, 0, st, p); \
+                     else hipLaunchKernelGGL((attention_kernel<D, TERMS, NT, false>), grid, block, 0, st, p)
+    if constexpr (D < 256)
+        if (plan.tiles16 == 2) { DYBIT_KV(2); return; }
+    DYBIT_KV(1);
+#undef DYBIT_KV
 }
 
 void launch(const Phase &p, const Plan &plan, int D, int terms, int64_t segments, hipStream_t st)
