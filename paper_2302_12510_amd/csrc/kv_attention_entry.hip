@@ -16,13 +16,14 @@ constexpr int kThreads = 256, kWaves = 4;
 // Up to kFew rows of a segment are tiles of 16 or 32 of a wave, whose waves share the keys of a chunk out; more go to the wide kernel,
 // whose waves share the rows out (64 sequences of 2048 tokens, 128 dims, 8 bits, us: 36 rows 100 as tiles, 132 wide; 64 rows 140, 134;
 // 96 rows 185, 135; 16 sequences, 256 dims: 64 rows 81, 104; 128 rows 141, 120).
-// The tokens of a segment go to workgroups in chunks: as many as the device holds workgroups at once (kHeld, by the kernels' registers;
-// kHeldWide waves), were all segments as long as the longest, since fewer leave it idle and more add their start and their partial
-// results (4 (D + 2) bytes a row, written and read back); twice as many behind a prefix, where there is a join anyway; but no longer ones
-// than kLongest for few rows, which keeps batches of very different lengths even.  Where tiles of the wide kernel alone are more
-// than the device holds (and nothing else is to be joined with them), they go whole, but for the last ones (Tile).
+// The tokens of a segment go to workgroups in chunks: two workgroups of four waves a compute unit (kHeld; kHeldWide waves of the wide
+// kernel), were all segments as long as the longest, since fewer leave the device idle and more add their start and their partial
+// results, 4 (D + 2) bytes a row, written and read back (one sequence of 128 Ki tokens: 384 workgroups 32.8 us, 512 28.9, 768 31.1);
+// three times as many behind a prefix, where there is a join anyway; but no longer ones than kLongest for few rows, which keeps batches
+// of very different lengths even.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be
+// joined with them), they go whole, but for the last ones (Tile).
 constexpr int64_t kFew = 64;
-constexpr int64_t kHeld = 768, kHeldWide = 2048;          // (waves, for the wide kernel)
+constexpr int64_t kHeld = 512, kHeldWide = 2048;
 constexpr int32_t kJoined = 512;                           // tokens behind a prefix that one workgroup joins with it
 constexpr int32_t kJoinedParts = 16;                       // and with so many parts of it: a wave takes a quarter of them, two at a time
 constexpr int32_t kShortest = 128, kLongest = 1536;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
@@ -39,7 +40,7 @@ Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, 
     const int64_t rows = p.wide ? kWideRows * waves : 16 * p.tiles16;
     p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
     const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
-    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide / waves : behind ? 2 * kHeld : kHeld) / base);
+    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide / waves : behind ? 3 * kHeld : kHeld) / base);
     int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
     chunk = std::max<int64_t>(chunk, kShortest);
     if (!p.wide) chunk = std::min<int64_t>(chunk, kLongest);
