@@ -101,8 +101,8 @@ __device__ __forceinline__ int visible(const Phase &p, const Segment &g, int i)
 // Tiles of rows that go to workgroups whole (Phase::whole).  The tiles of all segments, the last of a segment first, and of all key
 // heads, heads next to each other, fill the device's kCus workgroups some number of times; those left over, fewer than kCus, are cut
 // along the keys into as many parts as give all workgroups one (none, where they are more than half; kMostParts at most), so that the
-// last turn is a short one too.  Which
-// they are depends on the segments' numbers of queries, so workgroups find their tile themselves and leave word of it for the join.
+// last turn is a short one too.  Which they are depends on the segments' numbers of queries, so workgroups find their tile themselves and
+// leave word of it for the join.
 // Parts lie at [left-over tile][kMostParts][row of the tile].
 constexpr int kMostParts = 8;
 struct Left { int seg, head, tile, parts; };           // a left-over tile, for the join; the last one of kCus: how many there are (seg)

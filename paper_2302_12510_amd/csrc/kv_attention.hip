@@ -5,10 +5,14 @@
 // and the probabilities are rounded:
 //   - a row of queries is multiplied by the power of two that brings its largest element to [2^14, 2^15) and rounded to fp16 (16-bit
 //     types: exact but for elements 2^-28 below the largest), or, from fp32, split into a sum of two halves (22 bits);
-//   - a probability times its value's scale is divided by a power of two over the largest such scale seen so far, times 2^14,
+//   - a probability times its value's scale is divided by a power of two over the largest such scale seen so far, times 2^kLarge,
 //     and rounded to fp16 (fp32 outputs: two halves again).  The sum of the probabilities stays fp32 and unrounded.
 // The result of S^T (lane: one row, tokens 4 g + i) is the operand of O^T when its k slots are numbered that way, so probabilities
 // never change lanes.  Codes go from memory to registers to operands; no LDS in the loop.
+// Bound by memory where sequences are many and even (64 of 8192 tokens, 8 key heads of 128, 8 bits, 1.1 GB: 205 us, 5.4 TB/s; a device copy:
+// 5.1 of reads and writes), by the longest chunk where they are not (64 of 200 to 16 Ki, 474 MB: 106 us and 7 for the join), and by start
+// and join where there is one alone (128 Ki tokens, 4 key heads, 4 bits, 71 MB: 24 and 7 us,
+// 29 together).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -76,7 +80,8 @@ __global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void atten
         const int id = max(__builtin_amdgcn_readlane(page, ((step - wave) >> 1) + b), 0);
         return (((int64_t)id * p.kv_heads + head) << p.page_shift) + ((lo + 32 * step + 16 * b) & ((1 << p.page_shift) - 1));
     };
-    const unsigned klane = (unsigned)((lane & 15) * (D * KB / 8) + g4 * (D * KB / 32)), vlane = (unsigned)(4 * g4 * (D * VB / 8) + (lane & 15) * Vals<D>::BYTES);
+    const unsigned klane = (unsigned)((lane & 15) * (D * KB / 8) + g4 * (D * KB / 32));
+    const unsigned vlane = (unsigned)(4 * g4 * (D * VB / 8) + (lane & 15) * Vals<D>::BYTES);
     auto fetch_keys = [&](Keys<D> &k, int step) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -183,7 +188,8 @@ __global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void atten
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e ? a : first, prob[t][0][e], st[t].o[j], 0, 0, 0);
+                for (int e = 0; e < TERMS; ++e)
+                    st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e ? a : first, prob[t][0][e], st[t].o[j], 0, 0, 0);
         }
         if constexpr (decltype(more)::value) fetch_values(vals, step + kWaves);
     };

@@ -6,6 +6,12 @@
 // order (no bank conflicts, no padding); all of them read them all.  So decoding, some 2.5 instructions a code, is shared by the
 // rows of eight waves (four where a wave needs more than 256 registers).  The next step's codes are requested before this step's
 // products and decoded behind them, into the other half of the LDS.
+// Bound by the issue of vector instructions: 64 tokens for a wave's 32 rows of 128 dims are 64 matrix instructions (of 16 cycles on one of four
+// pipes: 1024) and some 350 others (four cycles each at least), a third of them decoding, the rest scales, maxima and exponentials.
+// Four prompts' chunks of 2048 tokens behind 4 to 8 Ki, 32 heads over 8 of 128 dims, 8 bits, 689 GFLOP: 870 us, 790 TFLOP/s; one of 2048
+// tokens on 32 Ki: 886 TFLOP/s; a bf16 library product of 8192^3 on the same card: 1310 to 1410.
+// Taken back, both sides measured, no gain: wave priorities round the products, half of the waves decoding before and half behind them
+// in every step, the operands of four products read ahead (2 to 8 % slower), two tiles' softmax and products woven into each other.
 #include <hip/hip_runtime.h>
 
 #include "kv_attention_rows.h"
@@ -169,7 +175,8 @@ __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void 
         float x[NT][N], sv[N];
 #pragma unroll
         for (int b = 0; b < kSubBlocks; ++b) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(&lds.sv[buffer][sub * kSub + 16 * b + 4 * g4]), k = *reinterpret_cast<const f32x4 *>(&lds.sk[buffer][sub * kSub + 16 * b + 4 * g4]);
+            const int at = sub * kSub + 16 * b + 4 * g4;
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(&lds.sv[buffer][at]), k = *reinterpret_cast<const f32x4 *>(&lds.sk[buffer][at]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 sv[4 * b + i] = v[i];
@@ -208,7 +215,8 @@ __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void 
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int e = 0; e < TERMS; ++e) st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e ? a : first, prob[t][c][e], st[t].o[j], 0, 0, 0);
+                    for (int e = 0; e < TERMS; ++e)
+                        st[t].o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e ? a : first, prob[t][c][e], st[t].o[j], 0, 0, 0);
             }
     };
     auto prepare = [&](int step) {                       // codes of `step` are in registers
@@ -233,7 +241,8 @@ __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void 
     for (int t = 0; t < NT; ++t) {
         settle<VB, TERMS>(st[t], r[t].factor, ref);
         if (r[t].row < 0) continue;
-        const int64_t at = p.whole ? ((int64_t)tile.left * kMostParts + tile.part) * ROWS + 16 * (NT * wave + t) + (lane & 15) : r[t].row * p.slots + p.slot0 + slot;
+        const int64_t at = p.whole ? ((int64_t)tile.left * kMostParts + tile.part) * ROWS + 16 * (NT * wave + t) + (lane & 15)
+                                   : r[t].row * p.slots + p.slot0 + slot;
         write_row<D>(p, r[t].row, parted ? at : -1, g4, st[t]);
     }
 }
@@ -241,7 +250,8 @@ __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void 
 template <int D>
 void launch_d(const Phase &p, const Plan &plan, int terms, int64_t segments, hipStream_t st)
 {
-    const dim3 grid = plan.whole ? dim3((unsigned)(plan.tiles + kCus)) : dim3((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots);
+    const dim3 grid = plan.whole ? dim3((unsigned)(plan.tiles + kCus))
+                                 : dim3((unsigned)(segments * p.kv_heads), (unsigned)plan.row_tiles, (unsigned)plan.slots);
     const dim3 block((unsigned)(64 * plan.waves));
     if constexpr (!wide_registers(D, 1))
         if (plan.waves == 8 && terms == 1) { hipLaunchKernelGGL((attention_wide_kernel<D, 1, 8>), grid, block, 0, st, p); return; }

@@ -15,6 +15,7 @@ constexpr int kThreads = 256;
 // A head's D elements lie in D / 8 lanes, eight each: the maximum goes round those lanes, each encodes its eight and stores one word
 // (4 bits) or two.  Before the encoder the head and its scale are multiplied by the power of two that brings the scale into [1, 2):
 // exact but for elements that underflow, whose code is 0 either way, and so any normal scale takes the encoder's one path.
+// Bound by memory: 16383 tokens of 8 heads of 128, fp32 to keys of 8 bits and values of 4, 161 MB in 34.0 us, 4.7 TB/s (a device copy: 5.1).
 struct AppendArgs {
     const void *x[2];
     int64_t token_stride[2], head_stride[2];
@@ -102,7 +103,8 @@ void launch_append(const AppendArgs &p, int D, bool vectors, hipStream_t st)
 
 // ---- copies of pages -------------------------------------------------------------------------------------------------------------
 // A page of a layer is four runs of whole 16-byte words (codes and scales of keys and of values); a workgroup moves a part of it,
-// every lane kUnroll words that are all requested before the first is stored.
+// every lane kUnroll words that are all requested before the first is stored.  Bound by memory: 511 pages in 16 layers, 2.21 GB, in
+// 438 us, 5.05 TB/s, a device copy's rate.
 struct CopyArgs {
     uint8_t *base[4];
     int64_t layer_bytes[4];             // from a layer's run to the next layer's
