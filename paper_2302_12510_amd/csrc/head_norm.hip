@@ -1,6 +1,6 @@
 // RMS norm of every query and key head with the rotation by the token's position, in one pass, and its gradient.
 //
-// A head is a list of D / 2 pairs: the rotated ones, then neighbours that pass unturned (a rotation with cos = 1, sin = 0).  A lane
+// A head is a list of D / 2 pairs: the rotated ones, then neighbours that pass unturned.  A lane
 // holds V consecutive pairs, 2 V elements in two vector accesses, so a rotation never leaves its lane; the lanes of a head share
 // only the sum of squares (and, backward, the sum of h x).  A wave takes the heads of one token side by side: its rows of the
 // cosine and sine tables, and the weights, are read once for all of them.
@@ -18,7 +18,7 @@
 namespace dybit {
 namespace headnorm {
 
-using heads::Pack;
+using heads::Loose;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostBlocks = 1024;                 // of the backward pass, whose partial sums of the weights' gradients are one row a block
@@ -34,10 +34,26 @@ struct Args {
     const float *cos, *sin;
     int64_t table_rows, tokens;
     int32_t D, half;                              // half: rotated pairs
-    int32_t neighbours, parts, lanes;             // parts: waves per token; lanes per head (a power of two)
+    int32_t neighbours, parts, lanes_log2;        // parts: waves per token; lanes per head, a power of two
+    int32_t turned, runs;                         // runs of V pairs of a head: the rotated ones, all of them
     float eps;
     int *err;
     float *partial;                               // [blocks][2][D]
+};
+
+// Runs of V pairs that cover a head, rotated pairs and the others apart.  Where V does not divide either number, its last run starts early:
+// the first `skip` pairs of it are the run's before as well, count once in the sums, and are stored twice, with one value (4000 tokens, 40
+// heads of 128 in fp16, 35 pairs of them rotated: 40 us, with pairs one by one 79).
+template <int V>
+struct Run {
+    int pair, skip;
+    __device__ __forceinline__ Run(const Args &p, int n)
+    {
+        const int from = n < p.turned ? 0 : p.half, all = n < p.turned ? p.half : p.D / 2 - p.half, at = (n < p.turned ? n : n - p.turned) * V;
+        const int first = min(at, all - V);
+        pair = n < p.runs ? from + first : p.D / 2;
+        skip = at - first;
+    }
 };
 
 // Where the V pairs from p on lie: their first and their second elements as two runs, or interleaved in one run of 2 V.
@@ -57,8 +73,8 @@ template <class T, int V>
 __device__ __forceinline__ void load_pairs(const T *row, const Place<V> &at, float (&a)[V], float (&b)[V])
 {
     float u[V], v[V];
-    Pack<T, V>::load(row + at.first, u);
-    Pack<T, V>::load(row + at.second, v);
+    Loose<T, V>::load(row + at.first, u);
+    Loose<T, V>::load(row + at.second, v);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const float s = 2 * i < V ? u[(2 * i) % V] : v[(2 * i) % V], t = 2 * i + 1 < V ? u[(2 * i + 1) % V] : v[(2 * i + 1) % V];
@@ -77,8 +93,8 @@ __device__ __forceinline__ void store_pairs(T *row, const Place<V> &at, const fl
         u[i] = at.woven ? s : a[i];
         v[i] = at.woven ? t : b[i];
     }
-    Pack<T, V>::store(row + at.first, u);
-    Pack<T, V>::store(row + at.second, v);
+    Loose<T, V>::store(row + at.first, u);
+    Loose<T, V>::store(row + at.second, v);
 }
 
 // Over a head's lanes (a power of two): lanes of a row of 16 by data-parallel permutes, rows by the rows' exchange.
@@ -98,15 +114,34 @@ __device__ __forceinline__ float sum_over(float x, int lanes)
     return x;
 }
 
+// A pair by its angle, or as it is (an infinite element behind the rotated ones is none of its neighbour's business).
+__device__ __forceinline__ void turn(float &a, float &b, float c, float s, bool turns)
+{
+    const float u = a * c - b * s, v = b * c + a * s;
+    a = turns ? u : a;
+    b = turns ? v : b;
+}
+
 // K: groups of V pairs per lane (1 except for heads that are wider than 64 lanes hold).
-template <class T, int V, int K, bool BACK>
+// OVER: some runs overlap (a variant of its own: the others would lose 2 % to it).
+template <class T, int V, int K, bool BACK, bool OVER>
 __global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int group = lane / p.lanes, groups = 64 / p.lanes, at = lane % p.lanes;
-    int pair[K];
+    const int lanes = 1 << p.lanes_log2, group = lane >> p.lanes_log2, groups = 64 >> p.lanes_log2, at = lane & (lanes - 1);
+    int pair[K], skip[K];
+    bool turns[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) pair[k] = (at + k * p.lanes) * V;
+    for (int k = 0; k < K; ++k) {
+        pair[k] = (at + k * lanes) * V;
+        skip[k] = 0;
+        if constexpr (OVER) {
+            const Run<V> run(p, at);
+            pair[k] = run.pair;
+            skip[k] = run.skip;
+        }
+        turns[k] = pair[k] < p.half;
+    }
     float dw[2][K][2 * V];
     if (BACK) {
 #pragma unroll
@@ -126,10 +161,10 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) { c[k][i] = known ? 1.0f : __builtin_nanf(""); s[k][i] = 0.0f; }
-            if (known && pair[k] < p.half) {
-                Pack<float, V>::load(p.cos + position * p.half + pair[k], c[k]);
-                Pack<float, V>::load(p.sin + position * p.half + pair[k], s[k]);
+            for (int i = 0; i < V; ++i) { c[k][i] = 1.0f; s[k][i] = 0.0f; }
+            if (known && turns[k]) {
+                Loose<float, V>::load(p.cos + position * p.half + pair[k], c[k]);
+                Loose<float, V>::load(p.sin + position * p.half + pair[k], s[k]);
             }
         }
         if (!known && lane == 0) *p.err = DYBIT_ERR_INVALID_ARG;
@@ -155,17 +190,24 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
                         for (int i = 0; i < V; ++i) {
                             squares += xa[k][i] * xa[k][i] + xb[k][i] * xb[k][i];
                             if (BACK) {
-                                const float u = ga[k][i] * c[k][i] + gb[k][i] * s[k][i], v = gb[k][i] * c[k][i] - ga[k][i] * s[k][i];
-                                ga[k][i] = u;
-                                gb[k][i] = v;
-                                dot += u * wa[k][i] * xa[k][i] + v * wb[k][i] * xb[k][i];
+                                turn(ga[k][i], gb[k][i], c[k][i], -s[k][i], turns[k]);
+                                dot += ga[k][i] * wa[k][i] * xa[k][i] + gb[k][i] * wb[k][i] * xb[k][i];
+                            }
+                        }
+                        if (OVER && skip[k]) {                        // K is 1: the sums are this run's alone
+                            squares = dot = 0.0f;
+#pragma unroll
+                            for (int i = 1; i < V; ++i) {
+                                if (i < skip[k]) continue;
+                                squares += xa[k][i] * xa[k][i] + xb[k][i] * xb[k][i];
+                                if (BACK) dot += ga[k][i] * wa[k][i] * xa[k][i] + gb[k][i] * wb[k][i] * xb[k][i];
                             }
                         }
                     }
                 }
-                squares = sum_over(squares, p.lanes);
-                if (BACK) dot = sum_over(dot, p.lanes);
-                const float r = 1.0f / __builtin_sqrtf(squares / (float)p.D + p.eps);
+                squares = sum_over(squares, lanes);
+                if (BACK) dot = sum_over(dot, lanes);
+                const float r = known ? 1.0f / __builtin_sqrtf(squares / (float)p.D + p.eps) : __builtin_nanf("");
                 const float pull = BACK ? dot / (float)p.D * r * r : 0.0f;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
@@ -181,9 +223,9 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
                                 dw[a][k][V + i] += gb[k][i] * (xb[k][i] * r);
                             }
                         } else {
-                            const float u = xa[k][i] * r * wa[k][i], v = xb[k][i] * r * wb[k][i];
-                            ya[i] = u * c[k][i] - v * s[k][i];
-                            yb[i] = v * c[k][i] + u * s[k][i];
+                            ya[i] = xa[k][i] * r * wa[k][i];
+                            yb[i] = xb[k][i] * r * wb[k][i];
+                            turn(ya[i], yb[i], c[k][i], s[k][i], turns[k]);
                         }
                     }
                     store_pairs<T, V>((T *)p.y[a] + t * p.yt[a] + h * p.yh[a], Place<V>(pair[k], p.half, p.neighbours), ya, yb);
@@ -201,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const Args p)
 #pragma unroll
             for (int i = 0; i < 2 * V; ++i) {
                 float x = dw[a][k][i];
-                for (int off = p.lanes; off < 64; off <<= 1) x += __shfl_xor(x, off);
+                for (int off = lanes; off < 64; off <<= 1) x += __shfl_xor(x, off);
                 dw[a][k][i] = x;
             }
             if (group == 0 && pair[k] < p.D / 2) {
@@ -259,34 +301,46 @@ int64_t backward_parts(int64_t tokens, int64_t turns)
 }
 int blocks_of(int64_t tokens, int64_t parts) { return (int)std::min<int64_t>(kMostBlocks, (tokens * parts + kWaves - 1) / kWaves); }
 
+// Waves of a token forward: about kForward in all, each with as many turns at the heads as the others.  More of them pay their start and
+// the token's row of the tables again, fewer leave the device idle (40 heads of 128 in bf16, us: 4096 tokens one wave a token 15.6, two
+// 16.5; 3000 tokens one 12.4, two 13.2, four 15.5; 1500 tokens one 9.6, two 8.7, four 10.0).
+constexpr int64_t kForward = 4096;
+int forward_parts(int64_t tokens, int turns)
+{
+    const int wanted = (int)std::min<int64_t>(turns, std::max<int64_t>(1, (kForward + tokens / 2) / std::max<int64_t>(1, tokens)));
+    const int rounds = (turns + wanted - 1) / wanted;
+    return (turns + rounds - 1) / rounds;
+}
+
 template <class T, bool BACK>
 int launch(Args &p, int V, hipStream_t st)
 {
     int blocks;
-    int lanes = 1;
-    while (lanes < 64 && lanes * V < p.D / 2) lanes *= 2;
-    p.lanes = lanes;
-    const int groups = 64 / lanes, turns = (p.heads[0] + groups - 1) / groups;
+    p.turned = (p.half + V - 1) / V;
+    p.runs = p.turned + (p.D / 2 - p.half + V - 1) / V;
+    const bool over = p.half % V || p.D / 2 % V;
+    while (p.lanes_log2 < 6 && 1 << p.lanes_log2 < p.runs) ++p.lanes_log2;
+    const int groups = 64 >> p.lanes_log2, turns = (p.heads[0] + groups - 1) / groups;
     if (BACK) {
         p.parts = (int)backward_parts(p.tokens, turns);
         blocks = blocks_of(p.tokens, p.parts);
     } else {
-        p.parts = p.tokens >= 4096 ? 1 : turns;
+        p.parts = forward_parts(p.tokens, std::max(1, turns));
         blocks = (int)((p.tokens * p.parts + kWaves - 1) / kWaves);
     }
     if (p.parts < 1) p.parts = 1;
     const dim3 grid((unsigned)blocks), block(kThreads);
-#define DYBIT_HN(V, K) hipLaunchKernelGGL((head_norm_kernel<T, V, K, BACK>), grid, block, 0, st, p)
+#define DYBIT_HN(V, K) \
+    if (over && V > 1) hipLaunchKernelGGL((head_norm_kernel<T, V, K, BACK, (V > 1)>), grid, block, 0, st, p); \
+    else hipLaunchKernelGGL((head_norm_kernel<T, V, K, BACK, false>), grid, block, 0, st, p)
     if constexpr (sizeof(T) == 2 && !BACK)
         if (V == 8) { DYBIT_HN(8, 1); return blocks; }
-    if (V == 4) DYBIT_HN(4, 1);
-    else if (V == 2) DYBIT_HN(2, 1);
-    else DYBIT_HN(1, 4);
+    if (V == 4) { DYBIT_HN(4, 1); }
+    else if (V == 2) { DYBIT_HN(2, 1); }
+    else { DYBIT_HN(1, 4); }
 #undef DYBIT_HN
     return blocks;
 }
-
-bool aligned_floats(const float *p, int n) { return reinterpret_cast<uintptr_t>(p) % (4u * (unsigned)n) == 0; }
 
 dybit_status run(bool back, const dybit_heads *g, const dybit_heads *x, const dybit_heads *y, const float *const *w, const int64_t *positions,
                  const float *cos_table, const float *sin_table, int64_t table_rows, int32_t rotary, int32_t neighbours, float eps,
@@ -314,10 +368,8 @@ dybit_status run(bool back, const dybit_heads *g, const dybit_heads *x, const dy
     // 128 in bf16, both passes: eight pairs 66 us, four 51)
     int V = x[0].type == DYBIT_F32 || back ? 4 : 8;
     auto fits = [&](int v) {
-        if ((D / 2) % v || (rotary / 2) % v || D / 2 > 64 * v || !aligned_floats(cos_table, v) || !aligned_floats(sin_table, v)) return false;
-        for (int a = 0; a < (keys ? 2 : 1); ++a)
-            if (!heads::aligned(x[a], v) || !heads::aligned(y[a], v) || (g && !heads::aligned(g[a], v)) || !aligned_floats(w[a], v)) return false;
-        return true;
+        const int turned = rotary / 2, rest = D / 2 - turned;
+        return turned >= v && (rest == 0 || rest >= v) && (turned + v - 1) / v + (rest + v - 1) / v <= 64;
     };
     while (V > 1 && !fits(V)) V /= 2;
     for (int a = 0; a < (keys ? 2 : 1); ++a) {

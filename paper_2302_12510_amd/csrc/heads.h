@@ -32,6 +32,25 @@ template <class T> struct Pack<T, 1> {
     static __device__ __forceinline__ void store(T *p, const float (&x)[1]) { *p = (T)x[0]; }
 };
 
+// The same from wherever an element may start: one access too, which the hardware splits where it crosses a line.
+template <class T, int V> struct Loose {
+    typedef T raw __attribute__((ext_vector_type(V), aligned(alignof(T))));
+    static __device__ __forceinline__ void load(const T *p, float (&x)[V])
+    {
+        const raw r = *reinterpret_cast<const raw *>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (float)r[i];
+    }
+    static __device__ __forceinline__ void store(T *p, const float (&x)[V])
+    {
+        raw r;
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = (T)x[i];               // one rounding, to nearest even
+        *reinterpret_cast<raw *>(p) = r;
+    }
+};
+template <class T> struct Loose<T, 1> : Pack<T, 1> {};
+
 inline int type_bytes(int type) { return type == DYBIT_F32 ? 4 : 2; }
 
 inline dybit_status check(const dybit_heads &h)

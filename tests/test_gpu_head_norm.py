@@ -174,3 +174,32 @@ def test_refusals():
         B.dybit_head_norm_rope(q, k, wq[:5], wk, positions, cos, sin)
     with pytest.raises(ValueError):
         B.dybit_head_norm_rope(q.transpose(1, 2), k, wq, wk, positions, cos, sin)
+
+
+@pytest.mark.parametrize("D,rot", [(64, 46), (80, 26), (96, 54), (128, 70), (256, 178), (512, 290), (64, 18), (96, 78), (34, 34), (50, 18)])
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_rotations_of_odd_widths(D, rot, dtype, neighbours):
+    """Pairs whose number the vector accesses do not divide, in heads that start anywhere, and in place."""
+    rng = np.random.default_rng(D * 1000 + rot)
+    args, ref = case(rng, 37, 7, 3, D, rot, dtype)
+    check(args, ref, dtype, neighbours, rng=rng, wrap=lambda t: inside_larger(t, pad=D % 3 + 1))
+    q, k, wq, wk, positions, cos, sin = args
+    gq, gk = (torch.randn(x.shape, generator=torch.Generator().manual_seed(rot)).to(x.dtype).cuda() for x in (q, k))
+    want = B.dybit_head_norm_rope(*args, 1e-6, neighbours), B.dybit_head_norm_rope_bwd(gq, gk, *args, 1e-6, neighbours)
+    mine = q.clone(), k.clone()
+    B.dybit_head_norm_rope(*mine, wq, wk, positions, cos, sin, 1e-6, neighbours, out=mine)
+    assert all(torch.equal(a, b) for a, b in zip(mine, want[0]))
+
+
+def test_an_infinite_element_of_overlapping_accesses():
+    """An infinite element makes its own head's elements zero or NaN as the formula does, whichever access reads it, and no other head's."""
+    rng = np.random.default_rng(11)
+    for at in range(64):
+        (q, k, wq, wk, positions, cos, sin), _ = case(rng, 2, 2, 1, 64, 46, "fp32")
+        q[0, 1, at] = float("inf")
+        got = B.dybit_head_norm_rope(q, k, wq, wk, positions, cos, sin)[0]
+        clean = torch.isfinite(got[0, 1])
+        touched = {at, at + 23 if at < 23 else at - 23 if at < 46 else at}
+        assert {int(i) for i in torch.nonzero(~clean)} == touched and bool((got[0, 1][clean] == 0).all())
+        assert bool(torch.isfinite(got[0, 0]).all() and torch.isfinite(got[1]).all())
