@@ -193,6 +193,8 @@ void launch_wide_k4v4(const Phase &p, const Plan &plan, int D, int terms, int64_
 // 8 key heads of 128 dims, 96 rows: eight 135 us, four 107; one sequence of 8192: 29 and 37, with twice the parts).
 constexpr int kWideRows = 32;
 constexpr bool wide_registers(int D, int terms) { return D * terms >= 256; }
+// The other kernel: where a wave needs more than 256 registers.
+constexpr bool narrow_registers(int D, int terms, int tiles16) { return D * tiles16 * terms >= 512; }
 constexpr int wide_waves(int D, int terms, int64_t most_rows, int64_t columns)
 {
     return wide_registers(D, terms) || (most_rows <= 4 * kWideRows && columns >= kCus) ? 4 : 8;

@@ -48,7 +48,7 @@ struct Vals {
 
 // JOINS: the rows are joined with what a shared prefix has left for them (in a kernel of its own: the others lose 2 to 7 % by it).
 template <int D, int TERMS, int NT, bool JOINS>
-__global__ __launch_bounds__(kThreads, D * NT * TERMS >= 512 ? 1 : 2) void attention_kernel(const Phase p)
+__global__ __launch_bounds__(kThreads, narrow_registers(D, TERMS, NT) ? 1 : 2) void attention_kernel(const Phase p)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     const int seg = (int)(blockIdx.x / (unsigned)p.kv_heads), head = (int)blockIdx.x - seg * p.kv_heads;

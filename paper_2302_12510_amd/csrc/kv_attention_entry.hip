@@ -19,8 +19,9 @@ constexpr int kThreads = 256, kWaves = 4;
 // The tokens of a segment go to workgroups in chunks: two workgroups of four waves a compute unit (kHeld; kHeldWide waves of the wide
 // kernel), were all segments as long as the longest, since fewer leave the device idle and more add their start and their partial
 // results, 4 (D + 2) bytes a row, written and read back (one sequence of 128 Ki tokens: 384 workgroups 32.8 us, 512 28.9, 768 31.1);
-// three times as many behind a prefix, where there is a join anyway; but no longer ones than kLongest for few rows, which keeps batches
-// of very different lengths even.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be
+// three times as many behind a prefix, where there is a join anyway; half as many where a wave needs the registers of two (us: 32 Ki
+// tokens of 256 dims, queries in fp32, 512 workgroups 43, 256 36; a group of 96 over a prefix, 384 rows of 256 dims, wide, 93 and 68); but
+// no longer ones than kLongest for few rows, twice that where half as many are held, which keeps batches of very different lengths even.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be
 // joined with them), they go whole, but for the last ones (Tile).
 constexpr int64_t kFew = 64;
 constexpr int64_t kHeld = 512, kHeldWide = 2048;
@@ -40,10 +41,12 @@ Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, 
     const int64_t rows = p.wide ? kWideRows * waves : 16 * p.tiles16;
     p.row_tiles = std::max<int64_t>(1, (max_rows + rows - 1) / rows);
     const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
-    const int64_t parts = std::max<int64_t>(1, (p.wide ? kHeldWide / waves : behind ? 3 * kHeld : kHeld) / base);
+    const bool alone = p.wide ? wide_registers(D, terms_of(type)) : narrow_registers(D, terms_of(type), p.tiles16);
+    const int64_t held = (p.wide ? kHeldWide / waves : behind ? 3 * kHeld : kHeld) / (alone ? 2 : 1);
+    const int64_t parts = std::max<int64_t>(1, held / base);
     int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
     chunk = std::max<int64_t>(chunk, kShortest);
-    if (!p.wide) chunk = std::min<int64_t>(chunk, kLongest);
+    if (!p.wide) chunk = std::min<int64_t>(chunk, alone ? 2 * kLongest : kLongest);
     // a segment's last tile may be part full: no more tiles than full ones of all rows there are and one a segment
     p.tiles = std::min(segments * p.row_tiles, all_rows / rows + segments) * kv_heads;
     p.whole = may_be_whole && p.wide && p.tiles >= kCus;
