@@ -21,12 +21,16 @@ constexpr int kThreads = 256, kWaves = 4;
 // results, 4 (D + 2) bytes a row, written and read back (one sequence of 128 Ki tokens: 384 workgroups 32.8 us, 512 28.9, 768 31.1);
 // three times as many behind a prefix, where there is a join anyway; half as many where a wave needs the registers of two (us: 32 Ki
 // tokens of 256 dims, queries in fp32, 512 workgroups 43, 256 36; a group of 96 over a prefix, 384 rows of 256 dims, wide, 93 and 68); but
-// no longer ones than kLongest for few rows, twice that where half as many are held, which keeps batches of very different lengths even.  Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be
-// joined with them), they go whole, but for the last ones (Tile).
+// no longer ones than kLongest for few rows, twice that where half as many are held, which keeps batches of very different lengths even.
+// For that the wide kernel's rounds are whole ones, of about kLongestWide tokens (12 sequences of 200 to 16 Ki with 96 rows, us: in one
+// round 229, 4096 125, 2048 135; 30 with 80 rows of 256 dims: 637, 335, 306; all of one length: 28 of 16 Ki 441, 485, 474; 12 234, 246, 210).
+// Where tiles of the wide kernel alone are more than the device holds (and nothing else is to be joined with them), they go whole, but for
+// the last ones (Tile).
 constexpr int64_t kFew = 64;
 constexpr int64_t kHeld = 512, kHeldWide = 2048;
 constexpr int32_t kJoined = 512;                           // tokens behind a prefix that one workgroup joins with it
 constexpr int32_t kJoinedParts = 16;                       // and with so many parts of it: a wave takes a quarter of them, two at a time
+constexpr int32_t kLongestWide = 2048;
 constexpr int32_t kShortest = 128, kLongest = 1536;       // (a wave can hold the pages of 64 blocks of 16 tokens, a quarter of 4096)
 
 // fp32 is split into two halves.
@@ -43,7 +47,8 @@ Plan plan_of(int64_t segments, int64_t max_rows, int kv_heads, int D, int type, 
     const int64_t base = std::max<int64_t>(1, segments * kv_heads * p.row_tiles);
     const bool alone = p.wide ? wide_registers(D, terms_of(type)) : narrow_registers(D, terms_of(type), p.tiles16);
     const int64_t held = (p.wide ? kHeldWide / waves : behind ? 3 * kHeld : kHeld) / (alone ? 2 : 1);
-    const int64_t parts = std::max<int64_t>(1, held / base);
+    int64_t parts = std::max<int64_t>(1, held / base);
+    if (p.wide) parts *= std::max<int64_t>(1, cap / (parts * kLongestWide));
     int64_t chunk = ((cap + parts - 1) / parts + kShortest - 1) / kShortest * kShortest;
     chunk = std::max<int64_t>(chunk, kShortest);
     if (!p.wide) chunk = std::min<int64_t>(chunk, alone ? 2 * kLongest : kLongest);

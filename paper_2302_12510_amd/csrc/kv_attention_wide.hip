@@ -28,7 +28,7 @@ namespace kv {
 namespace {
 
 constexpr int KB = DYBIT_KV_K, VB = DYBIT_KV_V;
-constexpr int NT = kWideRows / 16, kSub = 64, kSubBlocks = kSub / 16;     // tiles of a wave; tokens whose scores a wave holds at a time
+constexpr int NT = kWideRows / 16;                             // tiles of a wave
 
 // What a wave decodes of a step: the keys of 16 tokens, half the dims of the values of 32, and the scales of 16.
 template <int D>
@@ -52,7 +52,9 @@ struct Lds {
 template <int D, int TERMS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void attention_wide_kernel(const Phase p)
 {
-    constexpr int STEP = 16 * WAVES;
+    // tokens whose scores a wave holds at a time: 64, or 32 beside fp32 queries of 256 dims, which leave no registers for
+    // more (a prompt of 1724 tokens in three sequences of up to 5634, 16 heads over 8: 674 us with 64, which spill, 524 with 32)
+    constexpr int STEP = 16 * WAVES, kSub = D * TERMS >= 512 ? 32 : 64, kSubBlocks = kSub / 16;
     __shared__ Lds<D, WAVES> lds;                          // two buffers of 64 KB, or 32 for 64 dims
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4;
     constexpr int ROWS = 16 * NT * WAVES;
@@ -184,10 +186,15 @@ __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void 
                 for (int t = 0; t < NT; ++t) x[t][4 * b + i] = s[t][b][i] * k[i];
             }
         }
-        typedef int i32x4 __attribute__((ext_vector_type(4)));
-        const i32x4 valid = *reinterpret_cast<const i32x4 *>(&lds.valid[buffer][sub * kSubBlocks]);
-        const f32x4 tops = *reinterpret_cast<const f32x4 *>(&lds.top[buffer][sub * kSubBlocks]);
-        if (__builtin_amdgcn_readfirstlane(min(min(valid[0], valid[1]), min(valid[2], valid[3]))) < 16 || token + kSub > least) {
+        typedef int ints __attribute__((ext_vector_type(kSubBlocks)));
+        typedef float floats __attribute__((ext_vector_type(kSubBlocks)));
+        const ints valid = *reinterpret_cast<const ints *>(&lds.valid[buffer][sub * kSubBlocks]);
+        const floats tops = *reinterpret_cast<const floats *>(&lds.top[buffer][sub * kSubBlocks]);
+        int fewest = min(valid[0], valid[1]);
+        float top = fmaxf(tops[0], tops[1]);
+#pragma unroll
+        for (int b = 2; b < kSubBlocks; ++b) { fewest = min(fewest, valid[b]); top = fmaxf(top, tops[b]); }
+        if (__builtin_amdgcn_readfirstlane(fewest) < 16 || token + kSub > least) {
             // what lies past the end of the keys, or of what a row sees, counts nothing (the scales there are zero already)
             int at = 4 * g4;
             asm volatile("" : "+v"(at));                   // keeps all of it behind its branch: whole steps pay nothing
@@ -200,7 +207,7 @@ __global__ __launch_bounds__(64 * WAVES, wide_registers(D, TERMS) ? 1 : 2) void 
                     for (int i = 0; i < 4; ++i) x[t][4 * b + i] = i < left ? x[t][4 * b + i] : -__builtin_inff();
                 }
         }
-        const float shrink = ref.raise(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+        const float shrink = ref.raise(top);
         f16x8 prob[NT][N / 8][TERMS];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
