@@ -7,8 +7,8 @@
 //   forward   n = x r w,  r = 1 / sqrt(mean x^2 + eps),  y = R n
 //   backward  g' = R^T g,  h = g' w,  dx = r (h - x r^2 mean(h x)),  dw = sum g' x r
 // Both are bound by memory: a head is read and written once (backward: inputs and gradients read, written once).  8191 tokens of 40
-// heads of 128 in bf16, 171 MB: 39.5 us, 4.3 TB/s, where a device copy of as much takes 33; a training step of 4097 tokens of 32 heads of
-// 64 in fp32: 14 us forward, 22 us for its 101 MB backward, 4.6 to add the weights' partial gradients up.
+// heads of 128 in bf16, 171 MB: 34.0 to 39.5 us over cards, 4.3 to 5.0 TB/s, where a device copy of as much takes 33; a training step of
+// 4097 tokens of 32 heads of 64 in fp32: 14 us forward, 22 us for its 101 MB backward, 4.6 to add the weights' partial gradients up.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
