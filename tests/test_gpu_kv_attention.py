@@ -216,3 +216,19 @@ def test_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16"])
+@pytest.mark.parametrize("n", [1, 9, 40])
+def test_wide_heads_over_long_and_short_sequences(dtype, n):
+    """Few and many rows of 256 dims: workgroups that hold a compute unit alone, chunks in several rounds."""
+    rng = np.random.default_rng(n)
+    check_attention(rng, World(rng, [9000, 70, 1, 4100], 1, 256, (8, 4), 64), [n, min(n, 30), 1, n], 3, dtype)
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "fp32"), (256, "fp32"), (128, "bf16")])
+def test_many_short_sequences_beside_a_long_one(D, dtype):
+    """Nearly as many tiles as the device holds, of which one is long: it is cut into parts all the same."""
+    rng = np.random.default_rng(D)
+    lengths = [5200] + [int(x) for x in rng.integers(1, 60, 29)]
+    check_attention(rng, World(rng, lengths, 7, D, (4, 8), 32), [34] + [int(x) for x in rng.integers(0, 20, 29)], 14, dtype)
